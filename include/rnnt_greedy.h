@@ -61,7 +61,8 @@ enum {
     RNNT_ERR_HIP = -4,         /* a HIP runtime call failed                    */
     RNNT_ERR_UNSUPPORTED = -5, /* the device or the model does not fit         */
     RNNT_ERR_SCRATCH = -6      /* rnnt_label_looping_decode_noalloc: the call  */
-                               /* needs more than the static scratch array     */
+                               /* needs more than the static scratch array;    */
+                               /* operators: than the workspace it was given   */
 };
 
 /* Bits of the device status word (rnnt_engine_status). */
@@ -562,6 +563,123 @@ int rnnt_probe_e2m1_widening(float scale, uint16_t *bf16_out);
 int rnnt_probe_stream(int32_t from_l2, double *gbytes_per_s_out, double *per_cu_out);
 int rnnt_probe_exchange(int32_t team_size, int32_t len, int32_t tagged, double *us_per_exchange_out);
 int rnnt_probe_mfma(int32_t shape, double *tflops_out);
+
+/*
+ * Operators of a beam search whose products run on 4-bit operands: quantisation,
+ * product, selection over beams and vocabulary, reordering of states.  They need
+ * no engine.  All tensors are DEVICE memory of the current device; a call
+ * enqueues kernels on `stream` (of that device) and returns: it allocates
+ * nothing, reads nothing back, keeps nothing for the next call, and may be
+ * captured into a graph.  Errors are found on the host before anything is queued.
+ * Calls may overlap as long as they share no output and no workspace.  Outputs
+ * are the same bits from call to call on the same inputs.
+ *
+ * Types of tensors; strides and the counts of rows and columns are in elements,
+ * and a tensor's address is a multiple of its element's size (RNNT_ERR_SHAPE).
+ */
+#define RNNT_TYPE_F32 0
+#define RNNT_TYPE_BF16 1
+#define RNNT_TYPE_F16 2
+#define RNNT_TYPE_MX4 3       /* microscaled 4-bit: codes and scales, below     */
+
+/*
+ * Microscaled 4-bit matrices.  Every block of RNNT_MX4_BLOCK consecutive values
+ * of a row (the last one of a row may be shorter) is 2^k times OCP e2m1 values,
+ * k the smallest integer with max|block| * 2^-k <= 6, kept within +-127, 0 for
+ * a block of zeros: the rule of rnnt_quantize_blocks_e2m1 with the block length and
+ * the biased 8-bit exponents (k + 127) of the OCP microscaling formats.  Values
+ * are rounded to the nearest, ties to the even code.  A block that holds an infinity
+ * or a NaN has the exponent code 255 and stands for NaN as a whole.
+ *
+ * Layout, the one that the matrix instructions take their operands in.  codes:
+ * tiles of 16 rows by 128 columns, 1024 bytes each, row of tiles by row of tiles;
+ * in a tile the 16 bytes of block b (of 4), row r (of 16) are at (b * 16 + r) * 16,
+ * two codes a byte, the earlier column in the low half.  scales: for 16 rows by
+ * 512 columns 256 bytes, again row by row: the codes of block b, row r of the four
+ * tiles, in their order, are the four bytes at (b * 16 + r) * 4.  Rows are
+ * filled up to a multiple of 16 and columns to 128 (codes) and 512 (scales) with
+ * zeros times 2^0.  rnnt_mx4_sizes says how many bytes that is; *_out are HOST.
+ * codes are 16-byte and scales 4-byte aligned (else RNNT_ERR_SHAPE, as are
+ * negative counts; more than 2^31 - 1 rows or columns: RNNT_ERR_UNSUPPORTED).
+ */
+#define RNNT_MX4_BLOCK 32
+int rnnt_mx4_sizes(int64_t rows, int64_t cols, int64_t *codes_bytes_out, int64_t *scales_bytes_out);
+
+/*
+ * Quantise x [rows, cols] of `type` (F32, BF16 or F16), rows x_stride apart
+ * (>= cols).  values_out, if not NULL, is a dense float [rows, cols] that receives
+ * what the codes stand for (beyond the largest float: an infinity).  It may be x itself
+ * (a dense F32 one).  With rows or cols 0 nothing is done.
+ */
+int rnnt_mx4_quantize(const void *x, int32_t type, int64_t rows, int64_t cols, int64_t x_stride,
+                      void *codes_out, void *scales_out, float *values_out, rnnt_stream_t stream);
+
+/*
+ * y[m, n] = sum over k of Q(a)[m, k] * Q(w)[n, k] + bias[n], with fp32 sums.
+ *   a        [M, K]: of a_type F32, BF16 or F16 with rows a_stride apart, quantised
+ *            within the call (a_scales is not read), or the codes of an MX4
+ *            matrix, with its scales in a_scales (a_stride is not read)
+ *   w_codes, w_scales   [N, K] as rnnt_mx4_quantize lays it out
+ *   bias     [N] or NULL
+ *   y        [M, N] of y_type (F32, BF16 or F16; rounded once, ties to even), rows
+ *            y_stride apart (>= N); must not overlap the inputs
+ *   workspace  of at least rnnt_mx4_product_workspace bytes, 16-byte aligned,
+ *            or NULL where that is 0 (else RNNT_ERR_SCRATCH); its contents before
+ *            the call do not matter, and calls that overlap must not share it
+ * K = 0 gives the bias (a and w are not read), M = 0 or N = 0 nothing.
+ */
+int rnnt_mx4_product_workspace(int32_t a_type, int64_t M, int64_t N, int64_t K, int64_t *bytes_out);
+int rnnt_mx4_product(const void *a, const void *a_scales, int32_t a_type, int64_t a_stride,
+                     const void *w_codes, const void *w_scales, const float *bias,
+                     void *y, int32_t y_type, int64_t y_stride, int64_t M, int64_t N, int64_t K,
+                     void *workspace, int64_t workspace_bytes, rnnt_stream_t stream);
+
+/*
+ * A step of a beam search: the n_out best continuations of every utterance.  The
+ * candidate (k, v), token v behind hypothesis k, has the score
+ *   scores[b, k] + logits[b, k, v] - log(sum over u of exp(logits[b, k, u])),
+ * added up in 64 bits, the sum's terms in 32.  Candidates of an utterance go by their score, those of one
+ * hypothesis by their logit, and what ties by the lower k, then the lower v.
+ *   logits   [B, beams, V] of `type` (F32, BF16 or F16), strides in elements (>= 0; 0: the
+ *            same for all); a logit of -inf is no candidate
+ *   scores   [B, beams]: log-probabilities of the hypotheses so far; -inf for
+ *            one that does not exist, which has no candidates
+ *   finished [B, beams] or NULL: a hypothesis with a value other than 0 has one
+ *            candidate, end_token, at its own score; its logits are not used
+ *   scores_out, tokens_out, parents_out  [B, n_out]: score (rounded to fp32 at the end),
+ *            v and k, the best first; -inf, -1 and -1 where there are no
+ *            more candidates
+ * Candidates whose score is NaN do not count: a NaN among a hypothesis' logits, or
+ * +inf, leaves it without candidates.  1 <= beams <= 64, 1 <= n_out <= 64, V >= 1,
+ * 0 <= end_token < V where finished is given (else RNNT_ERR_SHAPE); beams * V below 2^31
+ * (else RNNT_ERR_UNSUPPORTED).  B = 0: nothing is done.  workspace: as above.
+ */
+int rnnt_beam_select_workspace(int32_t B, int32_t beams, int32_t V, int32_t n_out, int64_t *bytes_out);
+int rnnt_beam_select(const void *logits, int32_t type, int64_t batch_stride, int64_t beam_stride,
+                     const float *scores, const uint8_t *finished, int32_t B, int32_t beams, int32_t V,
+                     int32_t n_out, int32_t end_token, float *scores_out, int32_t *tokens_out,
+                     int32_t *parents_out, void *workspace, int64_t workspace_bytes, rnnt_stream_t stream);
+
+/*
+ * States follow the hypotheses: in up to RNNT_BEAM_STATES tensors at once,
+ *   dst[o, b, j, :] = src[o, b, parents[b, j], :]     o < outer, b < B, j < beams_out,
+ * rows of row_bytes bytes, strides in bytes.  parents [B, beams_out] as rnnt_beam_select
+ * writes it: where it is outside [0, beams_in) the row becomes zeros.  dst may be src
+ * (with the same strides and beams_in = beams_out); otherwise no destination row may overlap
+ * a source row or another destination row.  1 <= beams_in, beams_out <= 64, 1 <= n_states <=
+ * RNNT_BEAM_STATES, negative counts or strides, destination rows closer than row_bytes:
+ * RNNT_ERR_SHAPE.  `states` is a HOST array, read within the call.  B = 0: nothing is done.
+ */
+#define RNNT_BEAM_STATES 16
+typedef struct rnnt_beam_state {
+    const void *src;
+    void *dst;
+    int64_t outer, row_bytes;
+    int64_t src_outer, src_batch, src_beam;       /* strides                     */
+    int64_t dst_outer, dst_batch, dst_beam;
+} rnnt_beam_state;
+int rnnt_beam_reorder(const rnnt_beam_state *states, int32_t n_states, const int32_t *parents,
+                      int32_t B, int32_t beams_in, int32_t beams_out, rnnt_stream_t stream);
 
 /* Text for a return code; for RNNT_ERR_HIP includes the last HIP error text. */
 const char *rnnt_status_string(int code);

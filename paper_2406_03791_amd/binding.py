@@ -25,6 +25,8 @@ EXPORTS = (
     "rnnt_probe_stream", "rnnt_probe_exchange", "rnnt_probe_mfma", "rnnt_probe_e4m3_widening",
     "rnnt_quantize_rows_e4m3", "rnnt_quantize_blocks_e2m1", "rnnt_probe_e2m1_widening",
     "rnnt_probe_gate",
+    "rnnt_mx4_sizes", "rnnt_mx4_quantize", "rnnt_mx4_product_workspace", "rnnt_mx4_product",
+    "rnnt_beam_select_workspace", "rnnt_beam_select", "rnnt_beam_reorder",
 )
 
 
@@ -36,6 +38,10 @@ RNNT_FLAG_MULTI_BLANK = 16
 RNNT_FLAG_FP4_WEIGHTS = 32
 RNNT_FLAG_COOPERATIVE_LAUNCH = 128
 RNNT_FP4_BLOCK = 128
+RNNT_MX4_BLOCK = 32
+RNNT_BEAM_STATES = 16
+RNNT_TYPE_F32, RNNT_TYPE_BF16, RNNT_TYPE_F16, RNNT_TYPE_MX4 = 0, 1, 2, 3
+RNNT_TYPES = {"f32": RNNT_TYPE_F32, "bf16": RNNT_TYPE_BF16, "f16": RNNT_TYPE_F16, "mx4": RNNT_TYPE_MX4}
 
 
 class RnntError(RuntimeError):
@@ -56,6 +62,11 @@ class _ModelDesc(C.Structure):
         ("w_pred", C.c_void_p), ("b_pred", C.c_void_p),
         ("w_out", C.c_void_p), ("b_out", C.c_void_p),
     ]
+
+
+class _BeamState(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p)] + [(name, C.c_int64) for name in (
+        "outer", "row_bytes", "src_outer", "src_batch", "src_beam", "dst_outer", "dst_batch", "dst_beam")]
 
 
 class RnntStats(C.Structure):
@@ -124,6 +135,14 @@ def load_library():
                                            C.POINTER(C.c_float), C.POINTER(C.c_float)]
         lib.rnnt_probe_e2m1_widening.argtypes = [C.c_float, C.POINTER(C.c_uint16)]
         lib.rnnt_probe_gate.argtypes = [C.c_int32, C.POINTER(C.c_float), C.c_int64, C.POINTER(C.c_float)]
+        i32, i64, ptr, out64 = C.c_int32, C.c_int64, C.c_void_p, C.POINTER(C.c_int64)
+        lib.rnnt_mx4_sizes.argtypes = [i64, i64, out64, out64]
+        lib.rnnt_mx4_quantize.argtypes = [ptr, i32, i64, i64, i64, ptr, ptr, ptr, ptr]
+        lib.rnnt_mx4_product_workspace.argtypes = [i32, i64, i64, i64, out64]
+        lib.rnnt_mx4_product.argtypes = [ptr, ptr, i32, i64, ptr, ptr, ptr, ptr, i32, i64, i64, i64, i64, ptr, i64, ptr]
+        lib.rnnt_beam_select_workspace.argtypes = [i32, i32, i32, i32, out64]
+        lib.rnnt_beam_select.argtypes = [ptr, i32, i64, i64, ptr, ptr, i32, i32, i32, i32, i32, ptr, ptr, ptr, ptr, i64, ptr]
+        lib.rnnt_beam_reorder.argtypes = [C.POINTER(_BeamState), i32, ptr, i32, i32, i32, ptr]
         lib.rnnt_status_string.argtypes = [C.c_int]
         lib.rnnt_status_string.restype = C.c_char_p
         for name in EXPORTS:
@@ -320,6 +339,93 @@ def rnnt_probe_gate(is_tanh: bool, x):
     return out
 
 
+def rnnt_mx4_sizes(rows: int, cols: int):
+    """(bytes of the codes, bytes of the scales) of a microscaled 4-bit matrix."""
+    a, b = C.c_int64(0), C.c_int64(0)
+    _check(load_library().rnnt_mx4_sizes(rows, cols, C.byref(a), C.byref(b)))
+    return a.value, b.value
+
+
+def _a(t):
+    """A tensor's address as ctypes takes it."""
+    return None if t is None else t.data_ptr()
+
+
+def rnnt_mx4_quantize(x, type, rows, cols, x_stride, codes, scales, values=None, stream: int = 0) -> None:
+    _check(load_library().rnnt_mx4_quantize(_a(x), type, rows, cols, x_stride, _a(codes), _a(scales), _a(values),
+                                            stream or None))
+
+
+def rnnt_mx4_product_workspace(a_type: int, M: int, N: int, K: int) -> int:
+    out = C.c_int64(0)
+    _check(load_library().rnnt_mx4_product_workspace(a_type, M, N, K, C.byref(out)))
+    return out.value
+
+
+def rnnt_mx4_product(a, a_scales, a_type, a_stride, w_codes, w_scales, bias, y, y_type, y_stride, M, N, K,
+                     workspace=None, workspace_bytes=0, stream: int = 0) -> None:
+    _check(load_library().rnnt_mx4_product(_a(a), _a(a_scales), a_type, a_stride, _a(w_codes), _a(w_scales), _a(bias),
+                                           _a(y), y_type, y_stride, M, N, K, _a(workspace), workspace_bytes,
+                                           stream or None))
+
+
+def rnnt_beam_select_workspace(B: int, beams: int, V: int, n_out: int) -> int:
+    out = C.c_int64(0)
+    _check(load_library().rnnt_beam_select_workspace(B, beams, V, n_out, C.byref(out)))
+    return out.value
+
+
+def rnnt_beam_select(logits, type, batch_stride, beam_stride, scores, finished, B, beams, V, n_out, end_token,
+                     scores_out, tokens_out, parents_out, workspace=None, workspace_bytes=0, stream: int = 0) -> None:
+    _check(load_library().rnnt_beam_select(_a(logits), type, batch_stride, beam_stride, _a(scores), _a(finished),
+                                           B, beams, V, n_out, end_token, _a(scores_out), _a(tokens_out),
+                                           _a(parents_out), _a(workspace), workspace_bytes, stream or None))
+
+
+class BeamStates:
+    """What rnnt_beam_reorder moves: the C descriptors of pairs of tensors, and the tensors, kept alive."""
+
+    def __init__(self, pairs):
+        self.pairs = [(s, d) for s, d in pairs]
+        self.array = (_BeamState * max(1, len(self.pairs)))(*[_beam_state(s, d) for s, d in self.pairs])
+
+
+def _outer(t):
+    """(number, stride) of the rows of a tensor [..., B, beams, row] along its leading axes, which have to be as one."""
+    n, stride = 1, 0
+    for size, st in reversed(list(zip(t.shape[:-3], t.stride()[:-3]))):
+        if size == 1:
+            continue
+        if n > 1 and st != n * stride:
+            raise ValueError("the leading axes of a state have to have one stride between them")
+        n, stride = n * size, stride if n > 1 else st
+    return n, stride
+
+
+def _beam_state(src, dst):
+    if src.dim() < 3 or dst.dim() != src.dim() or src.dtype != dst.dtype or src.device != dst.device:
+        raise ValueError("states are pairs of tensors [..., B, beams, row] of one type on one device")
+    if src.shape[:-2] != dst.shape[:-2] or src.shape[-1] != dst.shape[-1]:
+        raise ValueError(f"states differ in more than the beams: {tuple(src.shape)} and {tuple(dst.shape)}")
+    if src.shape[-1] > 1 and (src.stride(-1) != 1 or dst.stride(-1) != 1):
+        raise ValueError("rows of a state have to be contiguous")
+    e, (n, so), (_, do) = src.element_size(), _outer(src), _outer(dst)
+    return _BeamState(src.data_ptr(), dst.data_ptr(), n if src.numel() or dst.numel() else 0, e * src.shape[-1],
+                      e * so, e * src.stride(-3), e * src.stride(-2), e * do, e * dst.stride(-3), e * dst.stride(-2))
+
+
+def rnnt_beam_states(pairs) -> BeamStates:
+    """Descriptors for rnnt_beam_reorder of (source, destination) tensors [..., B, beams, row]; a
+    destination may be its source."""
+    return BeamStates(pairs)
+
+
+def rnnt_beam_reorder(states, parents, B, beams_in, beams_out, stream: int = 0) -> None:
+    """states: of rnnt_beam_states, to be used again as long as the tensors stay where they are."""
+    _check(load_library().rnnt_beam_reorder(states.array, len(states.pairs), _a(parents), B, beams_in, beams_out,
+                                            stream or None))
+
+
 def rnnt_probe_mfma(shape: int) -> float:
     out = C.c_double(0)
     _check(load_library().rnnt_probe_mfma(int(shape), C.byref(out)))
@@ -424,3 +530,137 @@ class Engine:
 
     def phase_timers(self, team: int, n: int = 24):
         return rnnt_engine_phase_timers(self.handle, team, n)
+
+
+def _type_of(t) -> int:
+    name = {"torch.float32": "f32", "torch.bfloat16": "bf16", "torch.float16": "f16"}.get(str(t.dtype))
+    if name is None:
+        raise TypeError(f"float32, bfloat16 or float16 is wanted, not {t.dtype}")
+    return RNNT_TYPES[name]
+
+
+def _on_device(first, *others):
+    """The device of tensors that have to share one."""
+    if first.device.type != "cuda":
+        raise ValueError(f"tensors on the GPU are wanted, not on {first.device}")
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on one device are wanted, not on {first.device} and {t.device}")
+    return first.device
+
+
+def _rows_of(t, what: str):
+    """The row stride of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a matrix with contiguous rows is wanted")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+class Mx4Matrix:
+    """Owner of a microscaled 4-bit matrix [rows, cols]: codes and scales as rnnt_mx4_quantize lays them out.
+    Like Engine it holds no arithmetic: the methods allocate with torch, run on the current stream of the
+    tensors' device and forward to the C entry points."""
+
+    def __init__(self, rows: int, cols: int, device):
+        import torch
+        self.rows, self.cols = int(rows), int(cols)
+        codes, scales = rnnt_mx4_sizes(self.rows, self.cols)
+        self.codes = torch.empty(codes, dtype=torch.uint8, device=device)
+        self.scales = torch.empty(scales, dtype=torch.uint8, device=device)
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def quantize(self, x, values=None) -> "Mx4Matrix":
+        """Quantise x [rows, cols] (float32, bfloat16 or float16, contiguous rows) into this matrix; values: a
+        contiguous float32 tensor [rows, cols] for what the codes stand for."""
+        import torch
+        stride = _rows_of(x, "x")
+        if tuple(x.shape) != (self.rows, self.cols):
+            raise ValueError(f"x is {tuple(x.shape)}, the matrix {(self.rows, self.cols)}")
+        if values is not None and (values.dtype != torch.float32 or values.shape != x.shape or not values.is_contiguous()):
+            raise ValueError("values: a contiguous float32 tensor of the matrix' size is wanted")
+        with torch.cuda.device(_on_device(x, self.codes, values)):
+            rnnt_mx4_quantize(x, _type_of(x), self.rows, self.cols, stride, self.codes, self.scales, values,
+                              torch.cuda.current_stream().cuda_stream)
+        return self
+
+    def product(self, a, bias=None, out=None, dtype=None, workspace=None):
+        """Q(a) of this matrix transposed, plus bias [rows]: [M, rows] of `dtype` (float32 if not given) or in
+        `out`.  a: a tensor [M, cols] or an Mx4Matrix.  workspace: a uint8 tensor to be used instead of a new one."""
+        import torch
+        quantised = isinstance(a, Mx4Matrix)
+        M, cols = (a.rows, a.cols) if quantised else tuple(a.shape)
+        stride, a_type = (cols, RNNT_TYPE_MX4) if quantised else (_rows_of(a, "a"), _type_of(a))
+        codes, scales = (a.codes, a.scales) if quantised else (a, None)
+        if cols != self.cols:
+            raise ValueError(f"a has {cols} columns, the matrix {self.cols}")
+        if bias is not None and (bias.dtype != torch.float32 or tuple(bias.shape) != (self.rows,) or not bias.is_contiguous()):
+            raise ValueError("bias: a contiguous float32 vector of the matrix' rows is wanted")
+        device = _on_device(codes, scales, self.codes, bias, out, workspace)
+        if out is None:
+            out = torch.empty((M, self.rows), dtype=dtype or torch.float32, device=device)
+        elif tuple(out.shape) != (M, self.rows) or (dtype is not None and out.dtype != dtype):
+            raise ValueError(f"out: a {dtype or 'float'} matrix {(M, self.rows)} is wanted")
+        out_stride, out_type = _rows_of(out, "out"), _type_of(out)
+        need = rnnt_mx4_product_workspace(a_type, M, self.rows, self.cols)
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        with torch.cuda.device(device):
+            rnnt_mx4_product(codes, scales, a_type, stride, self.codes, self.scales, bias, out, out_type, out_stride,
+                             M, self.rows, self.cols, workspace, 0 if workspace is None else workspace.numel(),
+                             torch.cuda.current_stream().cuda_stream)
+        return out
+
+
+def mx4_quantize(x) -> Mx4Matrix:
+    """A new microscaled 4-bit copy of a matrix."""
+    return Mx4Matrix(x.shape[0], x.shape[1], x.device).quantize(x)
+
+
+def beam_select(logits, scores, n_out: Optional[int] = None, finished=None, end_token: int = 0, workspace=None):
+    """The n_out (by default as many as there are beams) best continuations of every utterance:
+    (scores, tokens, parents), tensors [B, n_out].  logits [B, beams, V], float32, bfloat16 or float16, contiguous
+    rows; scores [B, beams] float32; finished [B, beams] uint8 or bool (rnnt_beam_select)."""
+    import torch
+    if logits.dim() != 3 or (logits.shape[2] > 1 and logits.stride(2) != 1):
+        raise ValueError("logits: a tensor [B, beams, V] with contiguous rows is wanted")
+    B, beams, V = logits.shape
+    n_out = beams if n_out is None else int(n_out)
+    if scores.dtype != torch.float32 or tuple(scores.shape) != (B, beams) or not scores.is_contiguous():
+        raise ValueError("scores: a contiguous float32 tensor [B, beams] is wanted")
+    if finished is not None and (finished.dtype not in (torch.uint8, torch.bool) or tuple(finished.shape) != (B, beams)
+                                 or not finished.is_contiguous()):
+        raise ValueError("finished: a contiguous uint8 or bool tensor [B, beams] is wanted")
+    device = _on_device(logits, scores, finished, workspace)
+    need = rnnt_beam_select_workspace(B, beams, V, n_out)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    best = torch.empty((B, n_out), dtype=torch.float32, device=device)
+    tokens, parents = torch.empty((2, B, n_out), dtype=torch.int32, device=device)
+    with torch.cuda.device(device):
+        rnnt_beam_select(logits, _type_of(logits), logits.stride(0), logits.stride(1), scores, finished, B, beams, V,
+                         n_out, int(end_token), best, tokens, parents, workspace,
+                         0 if workspace is None else workspace.numel(), torch.cuda.current_stream().cuda_stream)
+    return best, tokens, parents
+
+
+def beam_reorder(pairs, parents) -> None:
+    """States follow the hypotheses: for every (source, destination) of `pairs` (or of a kept
+    rnnt_beam_states), tensors [..., B, beams, row], the destination's row of hypothesis j becomes the source's row of
+    hypothesis parents[b, j], zeros where there is none.  A destination may be its source."""
+    import torch
+    states = pairs if isinstance(pairs, BeamStates) else rnnt_beam_states(pairs)
+    if not states.pairs:
+        return
+    if parents.dtype != torch.int32 or parents.dim() != 2 or not parents.is_contiguous():
+        raise ValueError("parents: a contiguous int32 tensor [B, beams] is wanted")
+    (B, beams_out), beams_in = parents.shape, states.pairs[0][0].shape[-2]
+    device = _on_device(parents, *[t for pair in states.pairs for t in pair])
+    for src, dst in states.pairs:
+        if tuple(src.shape[-3:-1]) != (B, beams_in) or tuple(dst.shape[-3:-1]) != (B, beams_out):
+            raise ValueError(f"states of {B} utterances, {beams_in} and {beams_out} beams are wanted, not "
+                             f"{tuple(src.shape)} and {tuple(dst.shape)}")
+    with torch.cuda.device(device):
+        rnnt_beam_reorder(states, parents, B, beams_in, beams_out, torch.cuda.current_stream().cuda_stream)

@@ -1420,7 +1420,7 @@ const char *rnnt_status_string(int code)
     case RNNT_ERR_VARIANT: return "this decoder does not run this kind of model (RNN-T, TDT or multi-blank engine)";
     case RNNT_ERR_HIP: return g_hip_error.empty() ? "HIP runtime error" : g_hip_error.c_str();
     case RNNT_ERR_UNSUPPORTED: return "the device or the model shape is not supported";
-    case RNNT_ERR_SCRATCH: return "the call needs more scratch than the static array holds (RNNT_NOALLOC_SCRATCH_BYTES)";
+    case RNNT_ERR_SCRATCH: return "the call needs more scratch than the static array holds (RNNT_NOALLOC_SCRATCH_BYTES) or its workspace has";
     default: return "unknown status code";
     }
 }
