@@ -56,45 +56,136 @@ __device__ __forceinline__ v4u quantize_block(const float (&v)[32], unsigned &sc
     return c;
 }
 
-template <int TYPE>
-__device__ __forceinline__ void load_block(float (&v)[32], const void *x, long long row, long long rows, long long stride, long long col, long long cols)
+// N neighbours of a row, at any address that is a multiple of an element's size; zeros beyond the first `left`.
+template <class T, int N> struct Piece { T e[N]; };
+template <class T, int N>
+__device__ __forceinline__ Piece<T, N> load_piece(const T *p, long long left)
 {
-    typedef typename Element<TYPE>::T T;
-    const T *p = static_cast<const T *>(x) + row * stride + col;
-    const bool in = row < rows;
+    struct __attribute__((packed, aligned(sizeof(T)))) At { T e[N]; };
+    Piece<T, N> v;
+    if (left >= N) {
+        const At a = *reinterpret_cast<const At *>(p);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = in && col + i < cols ? (float)p[i] : 0.f;
+        for (int i = 0; i < N; ++i) v.e[i] = a.e[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v.e[i] = i < left ? p[i] : (T)0.f;
+    }
+    return v;
+}
+template <class T, int N>
+__device__ __forceinline__ void store_piece(T *p, const Piece<T, N> &v, long long left)
+{
+    struct __attribute__((packed, aligned(sizeof(T)))) At { T e[N]; };
+    if (left >= N) {
+        At a;
+#pragma unroll
+        for (int i = 0; i < N; ++i) a.e[i] = v.e[i];
+        *reinterpret_cast<At *>(p) = a;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) if (i < left) p[i] = v.e[i];
+    }
 }
 
-// A lane a block: what is beyond the matrix is quantised as zeros.
+// The block of 32 values at p of a row that goes on for `left` values from there
+template <class T>
+__device__ __forceinline__ void load_block(float (&v)[32], const T *p, long long left)
+{
+    constexpr int PER = 16 / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 32 / PER; ++i) {
+        const Piece<T, PER> a = load_piece<T, PER>(p + i * PER, left - i * PER);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) v[i * PER + e] = (float)a.e[e];
+    }
+}
+
+// The largest of the lanes that hold a block: 8 or 4 neighbours.
+template <int LANES>
+__device__ __forceinline__ unsigned block_top(unsigned m)
+{
+    m = max(m, (unsigned)__builtin_amdgcn_mov_dpp((int)m, 0xb1, 0xf, 0xf, true));                       // quad_perm [1,0,3,2]
+    m = max(m, (unsigned)__builtin_amdgcn_mov_dpp((int)m, 0x4e, 0xf, 0xf, true));                       // quad_perm [2,3,0,1]
+    if (LANES == 8) m = max(m, (unsigned)__builtin_amdgcn_mov_dpp((int)m, 0x141, 0xf, 0xf, true));      // row_half_mirror
+    return m;
+}
+
+// Memory bound: a work-group takes 16 rows by 512 columns, four rows a wave, and reads and writes whole lines: a lane
+// holds 16 bytes of a row, so that 8 lanes (16-bit types: 4) share a block and find its largest value in three (two) steps
+// between lanes.  Codes and scales are put in order in LDS and leave in one piece.
 template <int TYPE>
 __global__ void __launch_bounds__(256)
 mx4_quantize_kernel(const void *x, long long rows, long long cols, long long stride, unsigned char *codes, unsigned char *scales, float *values,
                     int col_tiles, int scale_tiles)
 {
-    const int lane = threadIdx.x & 63, r = lane & 15, b = lane >> 4;
-    const long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int across = scale_tiles * 4;                                // (scales go on to a multiple of four tiles)
-    const long long rt = i / across;
-    const int ct = (int)(i - rt * across);
-    if (rt >= tiles(rows, kTileRows)) return;
-    const long long row = rt * kTileRows + r, col = (long long)ct * kTileCols + b * RNNT_MX4_BLOCK;
-    float v[32];
-    load_block<TYPE>(v, x, row, rows, stride, col, cols);
-    unsigned scale;
-    const v4u c = quantize_block(v, scale);
-    if (ct < col_tiles) *reinterpret_cast<v4u *>(codes + (rt * col_tiles + ct) * kTileBytes + lane * 16) = c;
-    scales[(rt * scale_tiles + ct / 4) * kScaleBytes + lane * 4 + (ct & 3)] = (unsigned char)scale;
-    if (values && row < rows) {
-        const float unit = __uint_as_float(scale == 0u ? 0x00400000u : scale == 255u ? 0x7fc00000u : scale << 23);
+    typedef typename Element<TYPE>::T T;
+    constexpr int PER = 16 / sizeof(T), PARTS = kScaleCols / (64 * PER), LANES = RNNT_MX4_BLOCK / PER, ROWS = kTileRows / 4;
+    __shared__ __align__(16) unsigned char tile[4 * kTileBytes + kScaleBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int rt = blockIdx.x / scale_tiles, st = blockIdx.x - rt * scale_tiles;
+    const bool whole = (long long)(st + 1) * kScaleCols <= cols;
+    Piece<T, PER> v[ROWS][PARTS];
+    // (the same for all lanes: whether there is the row, and whether all its columns are inside)
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-            if (col + e >= cols) continue;
-            const unsigned code = c[e / 8] >> (e % 8 * 4) & 15u, m = code & 7u;
-            const float t = m < 4u ? 0.5f * (float)m : m == 4u ? 2.f : m == 5u ? 3.f : m == 6u ? 4.f : 6.f;
-            values[row * cols + col + e] = (code & 8u ? -t : t) * unit;
+    for (int i = 0; i < ROWS; ++i) {
+        const long long row = (long long)rt * kTileRows + wave * ROWS + i;
+        const T *p = static_cast<const T *>(x) + row * stride + (long long)st * kScaleCols + lane * PER;
+        const long long left = row < rows ? cols - (long long)st * kScaleCols - lane * PER : 0;
+        if (whole && row < rows) {
+#pragma unroll
+            for (int h = 0; h < PARTS; ++h) v[i][h] = load_piece<T, PER>(p + h * 64 * PER, PER);
+        } else {
+#pragma unroll
+            for (int h = 0; h < PARTS; ++h) v[i][h] = load_piece<T, PER>(p + h * 64 * PER, left - h * 64 * PER);
         }
     }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int r = wave * ROWS + i;
+#pragma unroll
+        for (int h = 0; h < PARTS; ++h) {
+            float f[PER];
+            unsigned top = 0;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) { f[e] = (float)v[i][h].e[e]; top = max(top, __float_as_uint(f[e]) & 0x7fffffffu); }
+            const unsigned scale = block_scale(block_top<LANES>(top));
+            const float unit = __uint_as_float(scale << 23);
+            unsigned c = 0;
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[0], f[1], unit, 0);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[2], f[3], unit, 1);
+            if constexpr (PER == 8) {
+                c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[4], f[5], unit, 2);
+                c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[6], f[7], unit, 3);
+            }
+            if (scale == 255u) c = 0;
+            const int in = (h * 64 + lane) * PER, t = in / kTileCols, b = in % kTileCols / RNNT_MX4_BLOCK;
+            unsigned char *to = tile + t * kTileBytes + (b * 16 + r) * 16 + in % RNNT_MX4_BLOCK / 2;
+            if constexpr (PER == 8) *reinterpret_cast<unsigned *>(to) = c;
+            else *reinterpret_cast<unsigned short *>(to) = (unsigned short)c;
+            if (lane % LANES == 0) tile[4 * kTileBytes + (b * 16 + r) * 4 + t] = (unsigned char)scale;
+            if (values) {
+                const long long row = (long long)rt * kTileRows + r, col = (long long)st * kScaleCols + in;
+                if (row >= rows || col >= cols) continue;
+                Piece<float, PER> o;
+#pragma unroll
+                for (int e = 0; e < PER; e += 2) {
+                    typedef float v2f __attribute__((ext_vector_type(2)));
+                    const unsigned pair = c >> (e * 4);
+                    const v2f two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(pair, unit, 0);
+                    o.e[e] = scale == 255u ? __uint_as_float(0x7fc00000u) : two.x;
+                    o.e[e + 1] = scale == 255u ? __uint_as_float(0x7fc00000u) : two.y;
+                }
+                store_piece<float, PER>(values + row * cols + col, o, whole ? PER : cols - col);
+            }
+        }
+    }
+    __syncthreads();
+    const int ct = st * 4 + wave;
+    if (ct < col_tiles)
+        *reinterpret_cast<v4u *>(codes + ((long long)rt * col_tiles + ct) * kTileBytes + lane * 16) = *reinterpret_cast<const v4u *>(tile + wave * kTileBytes + lane * 16);
+    if (wave == 0)
+        *reinterpret_cast<unsigned *>(scales + ((long long)rt * scale_tiles + st) * kScaleBytes + lane * 4) = *reinterpret_cast<const unsigned *>(tile + 4 * kTileBytes + lane * 4);
 }
 
 __device__ __forceinline__ void store(void *y, int type, long long at, float v)
@@ -126,7 +217,9 @@ mx4_product_kernel(const void *a, const unsigned char *a_scales, long long a_str
             as = a_scales[(mt * scale_tiles + s / 4) * kScaleBytes + lane * 4 + (s & 3)];
         } else {
             float v[32];
-            load_block<A>(v, a, mt * kTileRows + r, M, a_stride, (long long)s * kTileCols + b * RNNT_MX4_BLOCK, K);
+            typedef typename Element<A>::T T;
+            const long long row = mt * kTileRows + r, col = (long long)s * kTileCols + b * RNNT_MX4_BLOCK;
+            load_block<T>(v, static_cast<const T *>(a) + row * a_stride + col, row < M ? K - col : 0);
             ac = quantize_block(v, as);
         }
         const v8i wv = {(int)wc.x, (int)wc.y, (int)wc.z, (int)wc.w, 0, 0, 0, 0}, av = {(int)ac.x, (int)ac.y, (int)ac.z, (int)ac.w, 0, 0, 0, 0};
@@ -182,7 +275,7 @@ int rnnt_mx4_quantize(const void *x, int32_t type, int64_t rows, int64_t cols, i
     if (!x || !codes_out || !scales_out) return RNNT_ERR_NULL;
     if (!aligned(x, size_of(type)) || !aligned(codes_out, 16) || !aligned(scales_out, 4) || !aligned(values_out, 4)) return RNNT_ERR_SHAPE;
     const int ct = (int)tiles(cols, kTileCols), st = (int)tiles(cols, kScaleCols);
-    const long long blocks = tiles(tiles(rows, kTileRows) * st * 4, 4);
+    const long long blocks = tiles(rows, kTileRows) * st;
     if (blocks > kMost) return RNNT_ERR_UNSUPPORTED;
     auto run = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, static_cast<hipStream_t>(stream), x, (long long)rows, (long long)cols,
