@@ -5,11 +5,19 @@
 
 #include <math.h>
 
+#include <algorithm>
+
 #include "engine.h"
 
 namespace rnnt {
 
 constexpr int kMaxBeams = 64;
+constexpr int kTile = 1024;             // values of a row that a wave looks at together, 16 a lane
+constexpr int kPerLane = kTile / 64;
+constexpr int kBuffer = 128;            // candidates of a wave that wait to be sorted in
+constexpr int kJoinWaves = 16;          // waves of a work-group that joins lists, at most
+
+typedef unsigned long long u64;
 
 struct SelectArgs {
     const void *logits;
@@ -18,89 +26,355 @@ struct SelectArgs {
     float *scores_out;
     int *tokens_out, *parents_out;
     long long batch_stride, beam_stride;
-    int beams, V, n_out, end_token;
+    int B, beams, V, n_out, end_token;
+    int pieces, piece_tiles;            // a row is cut into so many pieces of so many tiles
+    u64 *lists;                         // [B][beams][pieces][n_out]: the pieces' best,
+    double *sums;                       // [B][beams][pieces]: sums of exponentials
+    float *tops;                        // and the logit that those are relative to (in the workspace; of one launch: in LDS)
 };
 
-template <int TYPE>
-__device__ __forceinline__ float logit(const void *p, long long at)
+// The value of lane ^ M
+template <int M> __device__ __forceinline__ unsigned from_lane(unsigned v)
 {
-    if constexpr (TYPE == RNNT_TYPE_F32) return static_cast<const float *>(p)[at];
-    else if constexpr (TYPE == RNNT_TYPE_BF16) return (float)static_cast<const __bf16 *>(p)[at];
-    else return (float)static_cast<const _Float16 *>(p)[at];
+#define RNNT_DPP(x, c) ((unsigned)__builtin_amdgcn_mov_dpp((int)(x), c, 0xf, 0xf, true))
+    if constexpr (M == 1) return RNNT_DPP(v, 0xb1);                           // quad_perm [1,0,3,2]
+    else if constexpr (M == 2) return RNNT_DPP(v, 0x4e);                      // quad_perm [2,3,0,1]
+    else if constexpr (M == 4) return RNNT_DPP(RNNT_DPP(v, 0x141), 0x1b);     // row_half_mirror, then quad_perm [3,2,1,0]
+    else if constexpr (M == 8) return RNNT_DPP(v, 0x128);                     // row_ror:8
+    else if constexpr (M == 15) return RNNT_DPP(v, 0x140);                    // row_mirror
+    else if constexpr (M == 16) {
+        const auto both = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return threadIdx.x & 16 ? both[0] : both[1];
+    } else {
+        static_assert(M == 32, "a power of two below 64, or 15");
+        const auto both = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return threadIdx.x & 32 ? both[0] : both[1];
+    }
+#undef RNNT_DPP
+}
+template <int M> __device__ __forceinline__ float from_lane(float v) { return __uint_as_float(from_lane<M>(__float_as_uint(v))); }
+template <int M> __device__ __forceinline__ u64 from_lane(u64 v) { return (u64)from_lane<M>((unsigned)(v >> 32)) << 32 | from_lane<M>((unsigned)v); }
+template <int M> __device__ __forceinline__ double from_lane(double v) { return __builtin_bit_cast(double, from_lane<M>(__builtin_bit_cast(u64, v))); }
+
+// An item of a list of a row, best first: the logit's place in the order of floats, and below it the token's complement, so that
+// of equal logits the lower token is the larger number.  0: nothing.
+struct InRow {
+    u64 key;
+    __device__ __forceinline__ bool above(const InRow &o) const { return key > o.key; }
+    template <int M> __device__ __forceinline__ InRow lane() const { return {from_lane<M>(key)}; }
+};
+// An item of a list of an utterance: the score's place in the order of doubles (0: nothing), and the complement of where it
+// comes from, hypothesis * 64 + rank in its list.
+struct InAll {
+    u64 key;
+    unsigned from;
+    __device__ __forceinline__ bool above(const InAll &o) const { return key > o.key || (key == o.key && from > o.from); }
+    template <int M> __device__ __forceinline__ InAll lane() const { return {from_lane<M>(key), from_lane<M>(from)}; }
+};
+
+__device__ __forceinline__ u64 row_key(float x, int token)
+{
+    const unsigned u = __float_as_uint(x + 0.f);                       // (-0 becomes 0)
+    return (u64)(u ^ ((unsigned)((int)u >> 31) | 0x80000000u)) << 32 | ~(unsigned)token;
+}
+__device__ __forceinline__ float key_logit(u64 key)
+{
+    const unsigned o = (unsigned)(key >> 32);
+    return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
 
-// A work-group an utterance.  The largest logit and the sum of a hypothesis first, then winner by winner the best of
-// what comes behind the last one.
+// A step of a sorting network: of lanes M apart the one keeps the better item, which has its bit of M clear or, if not
+// `first_up`, set.
+template <int M, class Item> __device__ __forceinline__ void exchange(Item &mine, bool better)
+{
+    const Item other = mine.template lane<M>();
+    const bool take = other.above(mine) == better;
+    if (take) mine = other;
+}
+// The items of a wave, best first (UP: worst first)
+template <bool UP, class Item> __device__ __forceinline__ void sort_wave(Item &v)
+{
+    const int lane = threadIdx.x & 63;
+#define RNNT_STEP(K, M) exchange<M>(v, (((lane & M) == 0) == ((lane & K) == 0)) != UP)
+    RNNT_STEP(2, 1);
+    RNNT_STEP(4, 2); RNNT_STEP(4, 1);
+    RNNT_STEP(8, 4); RNNT_STEP(8, 2); RNNT_STEP(8, 1);
+    RNNT_STEP(16, 8); RNNT_STEP(16, 4); RNNT_STEP(16, 2); RNNT_STEP(16, 1);
+    RNNT_STEP(32, 16); RNNT_STEP(32, 8); RNNT_STEP(32, 4); RNNT_STEP(32, 2); RNNT_STEP(32, 1);
+    RNNT_STEP(64, 32); RNNT_STEP(64, 16); RNNT_STEP(64, 8); RNNT_STEP(64, 4); RNNT_STEP(64, 2); RNNT_STEP(64, 1);
+#undef RNNT_STEP
+}
+// The best 64 of a sorted list and of another one that is given worst first, sorted
+template <class Item> __device__ __forceinline__ void join(Item &list, const Item &reversed)
+{
+    const int lane = threadIdx.x & 63;
+    if (reversed.above(list)) list = reversed;
+    exchange<32>(list, (lane & 32) == 0); exchange<16>(list, (lane & 16) == 0); exchange<8>(list, (lane & 8) == 0);
+    exchange<4>(list, (lane & 4) == 0); exchange<2>(list, (lane & 2) == 0); exchange<1>(list, (lane & 1) == 0);
+}
+template <class Item> __device__ __forceinline__ Item reverse(const Item &v) { return v.template lane<15>().template lane<16>().template lane<32>(); }
+
+// What lanes of a wave wrote to LDS is there for the others
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+template <int TYPE> struct Logit;
+template <> struct Logit<RNNT_TYPE_F32> { typedef float T; };
+template <> struct Logit<RNNT_TYPE_BF16> { typedef __bf16 T; };
+template <> struct Logit<RNNT_TYPE_F16> { typedef _Float16 T; };
+
+// One pass over a piece of a row: the running maximum and sum of a softmax, a lane's own, and the best n of its logits.
+// A logit that is not above the n-th best so far goes by at the price of a comparison for a lane's 16; the others
+// are put into a buffer, which is sorted and joined with the list 64 at a time.  Before there is a list, the maxima of n or more
+// groups of lanes bound the n-th best from below.
+template <class T> struct Scan {
+    static constexpr int PER = 16 / sizeof(T), LOADS = kPerLane / PER;
+    struct __attribute__((packed, aligned(sizeof(T)))) At { T e[PER]; };
+    const T *row;
+    u64 *buffer;
+    int n, lane;
+    int count = 0;                 // in the buffer
+    float bar = -INFINITY;         // logits above it are looked at
+    float top = -3.402823466e38f;  // (never -inf: differences to it are numbers)
+    double sum = 0;
+    InRow list{0};
+
+    __device__ __forceinline__ void flush()
+    {
+        wave_sync();
+        InRow v{lane < count ? buffer[lane] : 0};
+        const u64 rest = lane + 64 < count ? buffer[lane + 64] : 0;
+        wave_sync();
+        buffer[lane] = rest;
+        count = max(count - 64, 0);
+        sort_wave<true>(v);
+        join(list, v);
+        const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(list.key >> 32), n - 1);
+        if (hi != 0u) bar = key_logit((u64)hi << 32);
+    }
+    __device__ __forceinline__ void append(float x, int token)
+    {
+        const bool in = x > bar;
+        const u64 all = __ballot(in);
+        if (in) buffer[count + __builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0u))] = row_key(x, token);
+        count += __popcll(all);
+    }
+    __device__ __forceinline__ void first_bar(float m)
+    {
+        float t = m;
+        if (n <= 8) t = fmaxf(t, from_lane<4>(t));
+        if (n <= 16) t = fmaxf(t, from_lane<2>(t));
+        if (n <= 32) t = fmaxf(t, from_lane<1>(t));
+        t = fminf(t, from_lane<32>(t)); t = fminf(t, from_lane<16>(t)); t = fminf(t, from_lane<8>(t));
+        if (n > 8) t = fminf(t, from_lane<4>(t));
+        if (n > 16) t = fminf(t, from_lane<2>(t));
+        if (n > 32) t = fminf(t, from_lane<1>(t));
+        // the next lower number: it is among the best itself
+        const unsigned u = __float_as_uint(t);
+        bar = t == -INFINITY ? t : __uint_as_float(t == 0.f ? 0x80000001u : t > 0.f ? u - 1u : u + 1u);
+    }
+    // token(i): where f[i] stands; again(j): the logits from base + j * 64 on, one a lane, for more candidates than the buffer takes
+    template <class Token>
+    __device__ __forceinline__ void take(const float (&f)[kPerLane], int base, int end, bool first, Token token)
+    {
+        float m = f[0];
+#pragma unroll
+        for (int i = 1; i < kPerLane; ++i) m = fmaxf(m, f[i]);
+        constexpr float kLog2E = 1.44269504f;
+        const float next = fmaxf(top, m);
+        float part = 0.f;
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i) part += __builtin_amdgcn_exp2f((f[i] - next) * kLog2E);
+        sum = sum * (double)__builtin_amdgcn_exp2f((top - next) * kLog2E) + (double)part;
+        top = next;
+        if (first) first_bar(m);
+        if (__ballot(m > bar) == 0ull) return;
+        int more = 0;
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i) more += __popcll(__ballot(f[i] > bar));
+        if (count + more <= kBuffer) {
+#pragma unroll
+            for (int i = 0; i < kPerLane; ++i) append(f[i], token(i));
+            if (count >= 64) flush();
+            if (count >= 64) flush();
+        } else {
+            for (int j = lane; j - lane < end - base; j += 64) {
+                append(j < end - base ? (float)row[base + j] : -INFINITY, base + j);
+                if (count >= 64) flush();
+            }
+        }
+    }
+    __device__ __forceinline__ void run(int from, int to)
+    {
+        At next[LOADS];
+        auto load = [&](int base) {
+#pragma unroll
+            for (int q = 0; q < LOADS; ++q) next[q] = *reinterpret_cast<const At *>(row + base + (q * 64 + lane) * PER);
+        };
+        int base = from;                                   // (tokens may go on to the largest int)
+        if (to - base >= kTile) load(base);
+        for (; to - base >= kTile; base += kTile) {
+            float f[kPerLane];
+#pragma unroll
+            for (int i = 0; i < kPerLane; ++i) f[i] = (float)next[i / PER].e[i % PER];
+            if (to - base >= 2 * kTile) load(base + kTile);
+            take(f, base, base + kTile, base == from, [&](int i) { return base + (i / PER * 64 + lane) * PER + i % PER; });
+        }
+        if (base < to) {
+            float f[kPerLane];
+#pragma unroll
+            for (int i = 0; i < kPerLane; ++i) {
+                const int j = i * 64 + lane;
+                const float x = (float)row[base + min(j, to - base - 1)];
+                f[i] = j < to - base ? x : -INFINITY;
+            }
+            take(f, base, to, base == from, [&](int i) { return base + i * 64 + lane; });
+        }
+        if (count > 0) flush();
+        // over the lanes
+        float all = top;
+        all = fmaxf(all, from_lane<1>(all)); all = fmaxf(all, from_lane<2>(all)); all = fmaxf(all, from_lane<4>(all));
+        all = fmaxf(all, from_lane<8>(all)); all = fmaxf(all, from_lane<16>(all)); all = fmaxf(all, from_lane<32>(all));
+        sum *= (double)__builtin_amdgcn_exp2f((top - all) * 1.44269504f);
+        sum += from_lane<1>(sum); sum += from_lane<2>(sum); sum += from_lane<4>(sum);
+        sum += from_lane<8>(sum); sum += from_lane<16>(sum); sum += from_lane<32>(sum);
+        top = all;
+    }
+};
+
+// Piece `at` (of [B][beams][pieces]) by a wave; `slot`: where in the tables its results go
 template <int TYPE>
-__global__ void __launch_bounds__(256)
+__device__ __forceinline__ void scan_piece(const SelectArgs &a, long long at, u64 *buffer, u64 *lists, double *sums, float *tops, long long slot)
+{
+    typedef typename Logit<TYPE>::T T;
+    const long long hyp = at / a.pieces;
+    const int piece = (int)(at - hyp * a.pieces);
+    const long long b = hyp / a.beams;
+    const int k = (int)(hyp - b * a.beams);
+    const int lane = threadIdx.x & 63;
+    // (nothing of a finished hypothesis, or of one that does not exist, is looked at again)
+    if ((a.finished && a.finished[hyp]) || a.scores[hyp] == -INFINITY) return;
+    Scan<T> s;
+    s.row = static_cast<const T *>(a.logits) + b * a.batch_stride + k * a.beam_stride;
+    s.buffer = buffer; s.n = a.n_out; s.lane = lane;
+    const long long from = (long long)piece * a.piece_tiles * kTile;
+    s.run((int)from, (int)min(from + (long long)a.piece_tiles * kTile, (long long)a.V));
+    if (lane < a.n_out) lists[slot * a.n_out + lane] = s.list.key;
+    if (lane == 0) { sums[slot] = s.sum; tops[slot] = s.top; }
+}
+
+// The lists of an utterance's rows become one, by the waves of a work-group: hypothesis by hypothesis with its scores, then
+// wave by wave.  tokens: [beams][n_out], tree: [waves][64] keys and as many words, in LDS.
+__device__ __forceinline__ void join_rows(const SelectArgs &a, int b, int waves, const u64 *lists, const double *sums, const float *tops,
+                                          int *tokens, u64 *tree_keys, unsigned *tree_from)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = a.n_out;
+    InAll best{0, 0};
+    for (int k = wave; k < a.beams; k += waves) {
+        const long long hyp = (long long)b * a.beams + k;
+        const float score = a.scores[hyp];
+        InRow list{0};
+        double base = -INFINITY;
+        float top = 0.f;
+        if (a.finished && a.finished[hyp]) {
+            base = (double)score;
+            if (lane == 0) list.key = row_key(0.f, a.end_token);
+        } else if (score > -INFINITY) {
+            const u64 *mine = lists + (long long)k * a.pieces * n;
+            list.key = lane < n ? mine[lane] : 0;
+            for (int s = 1; s < a.pieces; ++s) join(list, InRow{63 - lane < n ? mine[s * n + 63 - lane] : 0});
+            // of the pieces' sums: a lane a piece
+            top = lane < a.pieces ? tops[k * a.pieces + lane] : -3.402823466e38f;
+            float all = top;
+            all = fmaxf(all, from_lane<1>(all)); all = fmaxf(all, from_lane<2>(all)); all = fmaxf(all, from_lane<4>(all));
+            all = fmaxf(all, from_lane<8>(all)); all = fmaxf(all, from_lane<16>(all)); all = fmaxf(all, from_lane<32>(all));
+            double sum = lane < a.pieces ? sums[k * a.pieces + lane] * exp((double)top - (double)all) : 0.0;
+            sum += from_lane<1>(sum); sum += from_lane<2>(sum); sum += from_lane<4>(sum);
+            sum += from_lane<8>(sum); sum += from_lane<16>(sum); sum += from_lane<32>(sum);
+            top = all;
+            base = (double)score - log(sum);               // (NaN where the row holds a NaN or an infinity)
+        }
+        InAll item{0, ~(unsigned)(k * 64 + lane)};
+        if (list.key != 0) {
+            const double t = base + ((double)key_logit(list.key) - (double)top) + 0.0;
+            const u64 u = __builtin_bit_cast(u64, t);
+            if (t > -INFINITY) item.key = u >> 63 ? ~u : u | 0x8000000000000000ull;
+        }
+        if (lane < n) tokens[k * n + lane] = (int)~(unsigned)list.key;
+        if (k == wave) best = item;
+        else join(best, reverse(item));
+    }
+    for (int half = waves / 2; half > 0; half /= 2) {
+        if (wave >= half && wave < 2 * half) { tree_keys[wave * 64 + lane] = best.key; tree_from[wave * 64 + lane] = best.from; }
+        __syncthreads();
+        if (wave < half) join(best, InAll{tree_keys[(wave + half) * 64 + 63 - lane], tree_from[(wave + half) * 64 + 63 - lane]});
+    }
+    __syncthreads();                                       // (one wave alone: its tokens)
+    if (wave == 0 && lane < n) {
+        const long long o = (long long)b * n + lane;
+        const int from = (int)~best.from, k = from >> 6;
+        const u64 u = best.key >> 63 ? best.key ^ 0x8000000000000000ull : ~best.key;
+        a.scores_out[o] = best.key ? (float)__builtin_bit_cast(double, u) : -INFINITY;
+        a.tokens_out[o] = best.key ? tokens[k * n + (from & 63)] : -1;
+        a.parents_out[o] = best.key ? k : -1;
+    }
+}
+
+// Where LDS goes in a launch that scans and joins
+struct SelectLds {
+    size_t buffers, tokens, lists, sums, tops, bytes;
+    __host__ __device__ SelectLds(int waves, int beams, int pieces, int n)
+    {
+        buffers = 0;                                       // (and, when they have been read, the waves' lists)
+        lists = buffers + (size_t)waves * kBuffer * 8;
+        sums = lists + (size_t)beams * pieces * n * 8;
+        tops = sums + (size_t)beams * pieces * 8;
+        tokens = tops + (size_t)beams * pieces * 4;
+        bytes = tokens + (size_t)beams * n * 4;
+    }
+};
+
+// A work-group an utterance: its waves take its pieces in turn, and join them
+template <int TYPE>
+__global__ void __launch_bounds__(kJoinWaves * 64)
 beam_select_kernel(const SelectArgs a)
 {
-    __shared__ double base[kMaxBeams];                 // of a hypothesis: its score less the logarithm of the sum
-    __shared__ float top[kMaxBeams];
-    __shared__ double s_best[256];
-    __shared__ float s_logit[256];
-    __shared__ int s_at[256];
-    const int b = blockIdx.x, tid = threadIdx.x;
-    const float *scores = a.scores + (long long)b * a.beams;
-    for (int k = 0; k < a.beams; ++k) {
-        const long long row = b * a.batch_stride + k * a.beam_stride;
-        float m = -INFINITY;
-        bool nan = false;
-        for (int v = tid; v < a.V; v += 256) { const float x = logit<TYPE>(a.logits, row + v); nan = nan || x != x; m = fmaxf(m, x); }
-        s_logit[tid] = nan ? INFINITY : m;
-        __syncthreads();
-        for (int h = 128; h > 0; h >>= 1) { if (tid < h) s_logit[tid] = fmaxf(s_logit[tid], s_logit[tid + h]); __syncthreads(); }
-        m = s_logit[0];
-        double sum = 0;
-        if (m < INFINITY && m > -INFINITY)
-            for (int v = tid; v < a.V; v += 256) sum += exp((double)logit<TYPE>(a.logits, row + v) - (double)m);
-        s_best[tid] = sum;
-        __syncthreads();
-        for (int h = 128; h > 0; h >>= 1) { if (tid < h) s_best[tid] += s_best[tid + h]; __syncthreads(); }
-        // (no candidates: the score becomes -inf)
-        if (tid == 0) { top[k] = m; base[k] = m < INFINITY && m > -INFINITY ? (double)scores[k] - log(s_best[0]) : -INFINITY; }
-        __syncthreads();
-    }
-    double last = INFINITY;
-    float last_x = INFINITY;
-    int last_at = -1;
-    for (int i = 0; i < a.n_out; ++i) {
-        double best = -INFINITY;
-        float best_x = -INFINITY;
-        int best_at = -1;
-        auto offer = [&](double t, float x, int at) {
-            if (!(t > -INFINITY)) return;
-            auto before = [&](double t0, float x0, int at0, double t1, float x1, int at1) {
-                if (at0 / a.V == at1 / a.V) return x0 > x1 || (x0 == x1 && at0 < at1);
-                return t0 > t1 || (t0 == t1 && at0 < at1);
-            };
-            if (last_at >= 0 && !before(last, last_x, last_at, t, x, at)) return;
-            if (best_at < 0 || before(t, x, at, best, best_x, best_at)) { best = t; best_x = x; best_at = at; }
-        };
-        for (int k = 0; k < a.beams; ++k) {
-            if (a.finished && a.finished[(long long)b * a.beams + k]) {
-                if (tid == 0) offer((double)scores[k], 0.f, k * a.V + a.end_token);
-                continue;
-            }
-            const long long row = b * a.batch_stride + k * a.beam_stride;
-            for (int v = tid; v < a.V; v += 256) {
-                const float x = logit<TYPE>(a.logits, row + v);
-                if (x > -INFINITY) offer(base[k] + ((double)x - (double)top[k]), x, k * a.V + v);
-            }
-        }
-        s_best[tid] = best; s_logit[tid] = best_x; s_at[tid] = best_at;
-        __syncthreads();
-        for (int t = 0; t < 256; ++t) if (s_at[t] >= 0) offer(s_best[t], s_logit[t], s_at[t]);
-        __syncthreads();
-        if (tid == 0) {
-            const long long o = (long long)b * a.n_out + i;
-            a.scores_out[o] = best_at < 0 ? -INFINITY : (float)best;
-            a.tokens_out[o] = best_at < 0 ? -1 : best_at % a.V;
-            a.parents_out[o] = best_at < 0 ? -1 : best_at / a.V;
-        }
-        if (best_at < 0) { last = -INFINITY; last_x = -INFINITY; last_at = 0x7fffffff; }
-        else { last = best; last_x = best_x; last_at = best_at; }
-    }
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const SelectLds l(waves, a.beams, a.pieces, a.n_out);
+    u64 *lists = reinterpret_cast<u64 *>(lds + l.lists);
+    double *sums = reinterpret_cast<double *>(lds + l.sums);
+    float *tops = reinterpret_cast<float *>(lds + l.tops);
+    const int n = a.beams * a.pieces;
+    for (int i = wave; i < n; i += waves)
+        scan_piece<TYPE>(a, (long long)blockIdx.x * n + i, reinterpret_cast<u64 *>(lds + l.buffers) + wave * kBuffer, lists, sums, tops, i);
+    __syncthreads();
+    u64 *tree = reinterpret_cast<u64 *>(lds + l.buffers);
+    join_rows(a, blockIdx.x, waves, lists, sums, tops, reinterpret_cast<int *>(lds + l.tokens), tree, reinterpret_cast<unsigned *>(tree + waves * 64));
+}
+
+// Few utterances with long rows: pieces over the whole device, joined by a second launch
+template <int TYPE>
+__global__ void __launch_bounds__(256)
+beam_scan_kernel(const SelectArgs a)
+{
+    __shared__ u64 buffers[4][kBuffer];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const long long at = (long long)blockIdx.x * 4 + wave;
+    if (at < (long long)a.B * a.beams * a.pieces) scan_piece<TYPE>(a, at, buffers[wave], a.lists, a.sums, a.tops, at);
+}
+__global__ void __launch_bounds__(kJoinWaves * 64)
+beam_join_kernel(const SelectArgs a)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int waves = blockDim.x >> 6;
+    const long long at = (long long)blockIdx.x * a.beams * a.pieces;
+    u64 *tree = reinterpret_cast<u64 *>(lds);
+    unsigned *from = reinterpret_cast<unsigned *>(tree + waves * 64);
+    join_rows(a, blockIdx.x, waves, a.lists + at * a.n_out, a.sums + at, a.tops + at, reinterpret_cast<int *>(from + waves * 64), tree, from);
 }
 
 struct ReorderState {
@@ -172,6 +446,36 @@ namespace {
 
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+// How a selection is cut up.  One launch, a work-group an utterance, where that leaves its waves no more than kOneLaunchTiles
+// tiles each and all of it fits LDS: the second launch costs what a wave takes for several tiles.  Else pieces of two tiles or more, towards
+// sixteen waves on every compute unit.
+constexpr int kOneLaunchTiles = 4, kWavesWanted = 4096, kLdsMost = 64 * 1024;
+
+struct SelectPlan {
+    bool two = false;
+    int pieces = 1, piece_tiles = 1, waves = 1;
+    size_t lds = 0;
+    int64_t bytes = 0;
+    SelectPlan(int64_t B, int beams, int V, int n)
+    {
+        const int row = (V - 1) / kTile + 1;
+        auto cut = [&](int64_t into) {
+            piece_tiles = (int)((row + into - 1) / into);
+            pieces = (row + piece_tiles - 1) / piece_tiles;
+        };
+        auto waves_for = [&](int jobs) { waves = 1; while (waves < kJoinWaves && waves < jobs) waves *= 2; };
+        cut(std::max(1, kJoinWaves / beams));
+        waves_for(beams * pieces);
+        lds = SelectLds(waves, beams, pieces, n).bytes;
+        if ((beams * pieces + waves - 1) / waves * piece_tiles <= kOneLaunchTiles && lds <= kLdsMost) return;
+        two = true;
+        cut(std::min<int64_t>(std::max<int64_t>(kWavesWanted / (B * beams), 1), std::min(64, (row + 1) / 2)));
+        waves_for(beams);
+        lds = (size_t)waves * 64 * 12 + (size_t)beams * n * 4;
+        bytes = B * beams * pieces * (n * 8 + 12);
+    }
+};
+
 }  // namespace
 
 extern "C" {
@@ -181,7 +485,7 @@ int rnnt_beam_select_workspace(int32_t B, int32_t beams, int32_t V, int32_t n_ou
     if (!bytes_out) return RNNT_ERR_NULL;
     if (B < 0 || beams < 1 || beams > kMaxBeams || V < 1 || n_out < 1 || n_out > kMaxBeams) return RNNT_ERR_SHAPE;
     if ((int64_t)beams * V > 0x7fffffff) return RNNT_ERR_UNSUPPORTED;
-    *bytes_out = 0;
+    *bytes_out = B > 0 ? SelectPlan(B, beams, V, n_out).bytes : 0;
     return RNNT_OK;
 }
 
@@ -200,11 +504,29 @@ int rnnt_beam_select(const void *logits, int32_t type, int64_t batch_stride, int
     if (!aligned(logits, type == RNNT_TYPE_F32 ? 4 : 2) || !aligned(scores, 4) || !aligned(scores_out, 4) || !aligned(tokens_out, 4) ||
         !aligned(parents_out, 4)) return RNNT_ERR_SHAPE;
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return RNNT_ERR_SCRATCH;
-    const SelectArgs args{logits, scores, finished, scores_out, tokens_out, parents_out, batch_stride, beam_stride, beams, V, n_out, end_token};
-    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(B), dim3(256), 0, static_cast<hipStream_t>(stream), args); };
-    if (type == RNNT_TYPE_F32) run(beam_select_kernel<RNNT_TYPE_F32>);
-    else if (type == RNNT_TYPE_BF16) run(beam_select_kernel<RNNT_TYPE_BF16>);
-    else run(beam_select_kernel<RNNT_TYPE_F16>);
+    const SelectPlan p(B, beams, V, n_out);
+    SelectArgs args{logits, scores, finished, scores_out, tokens_out, parents_out, batch_stride, beam_stride, B, beams, V, n_out, end_token,
+                    p.pieces, p.piece_tiles, nullptr, nullptr, nullptr};
+    const hipStream_t on = static_cast<hipStream_t>(stream);
+    if (!p.two) {
+        auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(B), dim3(p.waves * 64), (unsigned)p.lds, on, args); };
+        if (type == RNNT_TYPE_F32) run(beam_select_kernel<RNNT_TYPE_F32>);
+        else if (type == RNNT_TYPE_BF16) run(beam_select_kernel<RNNT_TYPE_BF16>);
+        else run(beam_select_kernel<RNNT_TYPE_F16>);
+        BEAM_TRY(hipGetLastError());
+        return RNNT_OK;
+    }
+    const int64_t n = (int64_t)B * beams * p.pieces;
+    args.lists = static_cast<u64 *>(workspace);
+    args.sums = reinterpret_cast<double *>(args.lists + n * n_out);
+    args.tops = reinterpret_cast<float *>(args.sums + n);
+    if ((n + 3) / 4 > 0x7fffffff) return RNNT_ERR_UNSUPPORTED;
+    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, on, args); };
+    if (type == RNNT_TYPE_F32) run(beam_scan_kernel<RNNT_TYPE_F32>);
+    else if (type == RNNT_TYPE_BF16) run(beam_scan_kernel<RNNT_TYPE_BF16>);
+    else run(beam_scan_kernel<RNNT_TYPE_F16>);
+    BEAM_TRY(hipGetLastError());
+    hipLaunchKernelGGL(beam_join_kernel, dim3(B), dim3(p.waves * 64), (unsigned)p.lds, on, args);
     BEAM_TRY(hipGetLastError());
     return RNNT_OK;
 }
