@@ -377,13 +377,18 @@ beam_join_kernel(const SelectArgs a)
     join_rows(a, blockIdx.x, waves, a.lists + at * a.n_out, a.sums + at, a.tops + at, reinterpret_cast<int *>(from + waves * 64), tree, from);
 }
 
+// A state as the reorder kernel moves it: rows in columns of `width` bytes.  Out of place a work-group takes kItems
+// columns of all rows of an utterance (of one o), row behind row; in place the same 256 columns of every row.
+constexpr int kUnroll = 8, kItems = 256 * kUnroll;
 struct ReorderState {
     const char *src;
     char *dst;
     long long src_outer, src_batch, src_beam, dst_outer, dst_batch, dst_beam;
-    unsigned columns;       // a row in pieces of `width` bytes
-    unsigned width, first;  // first: its first work-group
-    unsigned chunks;        // work-groups a row set
+    unsigned columns, width;
+    unsigned first;         // its first work-group
+    unsigned chunks;        // work-groups of an utterance
+    unsigned inverse;       // 2^32 / columns, rounded up, where there are fewer columns than kItems
+    unsigned in_place;
 };
 struct ReorderArgs {
     ReorderState s[RNNT_BEAM_STATES];
@@ -391,44 +396,100 @@ struct ReorderArgs {
     int n, B, beams_in, beams_out;
 };
 
-// A thread moves one column of all hypotheses of an utterance: every source is read before the first
-// destination is written, so that a state may be moved within itself.
-template <class T, int BEAMS>
-__device__ __forceinline__ void reorder_columns(const ReorderState &s, const int *parents, unsigned c, long long o, long long b, int beams_in, int beams_out)
+typedef unsigned v2u __attribute__((ext_vector_type(2)));
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
+
+// Memory bound.  Eight loads of a thread are on their way together, whatever rows they are of.
+template <class T>
+__device__ __forceinline__ void move_items(const ReorderState &s, const int *parents, unsigned chunk, long long o, long long b, int beams_in, int beams_out)
 {
-    const char *from = s.src + o * s.src_outer + b * s.src_batch + (long long)c * sizeof(T);
-    char *to = s.dst + o * s.dst_outer + b * s.dst_batch + (long long)c * sizeof(T);
+    const char *from = s.src + o * s.src_outer + b * s.src_batch;
+    char *to = s.dst + o * s.dst_outer + b * s.dst_batch;
+    const unsigned long long start = (unsigned long long)chunk * kItems;
+    unsigned row0 = 0;                                     // start / columns, bit by bit
+#pragma unroll
+    for (unsigned bit = kMaxBeams / 2; bit > 0; bit /= 2) if ((unsigned long long)(row0 + bit) * s.columns <= start) row0 += bit;
+    const unsigned col0 = (unsigned)(start - (unsigned long long)row0 * s.columns);
+    // row and column of the thread's i-th item.  (With fewer than kItems columns the number below is under 2 kItems, and the
+    // quotient by the inverse exact; with more it is under two rows.)
+    auto item = [&](int i, unsigned &j, unsigned &c) {
+        const unsigned at = col0 + i * 256 + threadIdx.x;
+        const unsigned down = s.columns >= (unsigned)kItems ? (at >= s.columns ? 1u : 0u) : s.columns > 1 ? __umulhi(at, s.inverse) : at;
+        j = row0 + down;
+        c = at - down * s.columns;
+    };
+    T v[kUnroll];
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i) {
+        unsigned j, c;
+        item(i, j, c);
+        // (where there is no source, the first row's column stands in: no branch around a load)
+        const bool in = j < (unsigned)beams_out;
+        const int p = parents[in ? j : 0u];
+        const bool there = in && p >= 0 && p < beams_in;
+        v[i] = *reinterpret_cast<const T *>(from + (there ? p * s.src_beam : 0ll) + (unsigned long long)(in ? c : 0u) * sizeof(T));
+        if (!there) v[i] = T{};
+    }
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i) {
+        unsigned j, c;
+        item(i, j, c);
+        if (j < (unsigned)beams_out) *reinterpret_cast<T *>(to + j * s.dst_beam + (unsigned long long)c * sizeof(T)) = v[i];
+    }
+}
+
+// Within itself: a thread has one column of all rows, and has read every source before it writes.  A row that stays where it
+// is, is left alone.
+template <class T, int BEAMS>
+__device__ __forceinline__ void move_within(const ReorderState &s, const int *parents, unsigned c, long long o, long long b, int beams)
+{
+    if (c >= s.columns) return;
+    char *at = s.dst + o * s.dst_outer + b * s.dst_batch + (unsigned long long)c * sizeof(T);
+    // (no branch around a load: where there is no source, or no such row, a row that there is stands in)
     T v[BEAMS];
 #pragma unroll
     for (int j = 0; j < BEAMS; ++j) {
-        v[j] = T{};
-        if (j >= beams_out) continue;
-        const int p = parents[j];
-        if (p >= 0 && p < beams_in) v[j] = *reinterpret_cast<const T *>(from + p * s.src_beam);
+        const int row = min(j, beams - 1), p = parents[row];
+        const bool there = p >= 0 && p < beams;
+        v[j] = *reinterpret_cast<const T *>(at + (there ? p : row) * s.dst_beam);
+        if (!there) v[j] = T{};
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
     for (int j = 0; j < BEAMS; ++j)
-        if (j < beams_out) *reinterpret_cast<T *>(to + j * s.dst_beam) = v[j];
+        if (j < beams && parents[j] != j) *reinterpret_cast<T *>(at + j * s.dst_beam) = v[j];
 }
 
+// BEAMS: room for the rows of an utterance that is moved within itself (0: no state is)
 template <int BEAMS>
 __global__ void __launch_bounds__(256)
 beam_reorder_kernel(const ReorderArgs a)
 {
-    typedef unsigned v2u __attribute__((ext_vector_type(2)));
     int i = 0;
     while (i + 1 < a.n && blockIdx.x >= a.s[i + 1].first) ++i;
     const ReorderState &s = a.s[i];
-    const unsigned at = blockIdx.x - s.first, set = at / s.chunks, c = (at - set * s.chunks) * 256 + threadIdx.x;
+    const unsigned at = blockIdx.x - s.first, set = at / s.chunks, chunk = at - set * s.chunks;
     const long long o = set / a.B, b = set - o * a.B;
-    if (c >= s.columns) return;
     const int *parents = a.parents + b * a.beams_out;
+    if constexpr (BEAMS > 0) {
+        if (s.in_place) {
+            const unsigned c = chunk * 256 + threadIdx.x;
+            switch (s.width) {
+            case 16: if constexpr (BEAMS <= 16) move_within<v4u, BEAMS>(s, parents, c, o, b, a.beams_out); break;
+            case 8: move_within<v2u, BEAMS>(s, parents, c, o, b, a.beams_out); break;
+            case 4: move_within<unsigned, BEAMS>(s, parents, c, o, b, a.beams_out); break;
+            case 2: move_within<unsigned short, BEAMS>(s, parents, c, o, b, a.beams_out); break;
+            default: move_within<unsigned char, BEAMS>(s, parents, c, o, b, a.beams_out); break;
+            }
+            return;
+        }
+    }
     switch (s.width) {
-    case 8: reorder_columns<v2u, BEAMS>(s, parents, c, o, b, a.beams_in, a.beams_out); break;
-    case 4: reorder_columns<unsigned, BEAMS>(s, parents, c, o, b, a.beams_in, a.beams_out); break;
-    case 2: reorder_columns<unsigned short, BEAMS>(s, parents, c, o, b, a.beams_in, a.beams_out); break;
-    default: reorder_columns<unsigned char, BEAMS>(s, parents, c, o, b, a.beams_in, a.beams_out); break;
+    case 16: move_items<v4u>(s, parents, chunk, o, b, a.beams_in, a.beams_out); break;
+    case 8: move_items<v2u>(s, parents, chunk, o, b, a.beams_in, a.beams_out); break;
+    case 4: move_items<unsigned>(s, parents, chunk, o, b, a.beams_in, a.beams_out); break;
+    case 2: move_items<unsigned short>(s, parents, chunk, o, b, a.beams_in, a.beams_out); break;
+    default: move_items<unsigned char>(s, parents, chunk, o, b, a.beams_in, a.beams_out); break;
     }
 }
 
@@ -542,6 +603,7 @@ int rnnt_beam_reorder(const rnnt_beam_state *states, int32_t n_states, const int
     args.parents = parents;
     args.B = B; args.beams_in = beams_in; args.beams_out = beams_out;
     int64_t groups = 0;
+    bool any_within = false;
     for (int i = 0; i < n_states; ++i) {
         const rnnt_beam_state &s = states[i];
         if (s.outer < 0 || s.row_bytes < 0 || s.src_outer < 0 || s.src_batch < 0 || s.src_beam < 0 || s.dst_outer < 0 || s.dst_batch < 0 || s.dst_beam < 0)
@@ -551,20 +613,25 @@ int rnnt_beam_reorder(const rnnt_beam_state *states, int32_t n_states, const int
             return RNNT_ERR_SHAPE;
         if (B == 0 || s.outer == 0 || s.row_bytes == 0) continue;
         if (!s.src || !s.dst || !parents) return RNNT_ERR_NULL;
-        // the widest piece that divides addresses, strides and rows
+        // the widest piece that divides addresses, strides and rows (in place, where a thread holds a column
+        // of all rows, with more than 16 rows 8 bytes)
+        const bool within = s.src == s.dst;
         const uint64_t all = reinterpret_cast<uintptr_t>(s.src) | reinterpret_cast<uintptr_t>(s.dst) | (uint64_t)s.row_bytes | (uint64_t)s.src_outer |
-                             (uint64_t)s.src_batch | (uint64_t)s.src_beam | (uint64_t)s.dst_outer | (uint64_t)s.dst_batch | (uint64_t)s.dst_beam | 8u;
+                             (uint64_t)s.src_batch | (uint64_t)s.src_beam | (uint64_t)s.dst_outer | (uint64_t)s.dst_batch | (uint64_t)s.dst_beam | (within && beams_out > 16 ? 8u : 16u);
         const unsigned width = (unsigned)(all & (~all + 1));
-        const int64_t columns = s.row_bytes / width, chunks = (columns + 255) / 256;
-        if (s.outer > 0x7fffffff / B || chunks > 0x7fffffff / (s.outer * B)) return RNNT_ERR_UNSUPPORTED;
+        const int64_t columns = s.row_bytes / width, chunks = within ? (columns + 255) / 256 : (columns * beams_out + kItems - 1) / kItems;
+        if (columns > 0x7fffffff - kItems || s.outer > 0x7fffffff / B || chunks > 0x7fffffff / (s.outer * B)) return RNNT_ERR_UNSUPPORTED;
         args.s[args.n++] = ReorderState{static_cast<const char *>(s.src), static_cast<char *>(s.dst), s.src_outer, s.src_batch, s.src_beam, s.dst_outer,
-                                        s.dst_batch, s.dst_beam, (unsigned)columns, width, (unsigned)groups, (unsigned)chunks};
+                                        s.dst_batch, s.dst_beam, (unsigned)columns, width, (unsigned)groups, (unsigned)chunks,
+                                        columns > 1 && columns < kItems ? (unsigned)(0x100000000ull / columns + 1) : 0u, within ? 1u : 0u};
+        any_within = any_within || within;
         groups += chunks * s.outer * B;
         if (groups > 0x7fffffff) return RNNT_ERR_UNSUPPORTED;
     }
     if (args.n == 0) return RNNT_OK;
     auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, static_cast<hipStream_t>(stream), args); };
-    if (beams_out <= 8) run(beam_reorder_kernel<8>);
+    if (!any_within) run(beam_reorder_kernel<0>);
+    else if (beams_out <= 8) run(beam_reorder_kernel<8>);
     else if (beams_out <= 16) run(beam_reorder_kernel<16>);
     else if (beams_out <= 32) run(beam_reorder_kernel<32>);
     else run(beam_reorder_kernel<64>);
