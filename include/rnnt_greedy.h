@@ -599,8 +599,8 @@ int rnnt_probe_mfma(int32_t shape, double *tflops_out);
  * tiles, in their order, are the four bytes at (b * 16 + r) * 4.  Rows are
  * filled up to a multiple of 16 and columns to 128 (codes) and 512 (scales) with
  * zeros times 2^0.  rnnt_mx4_sizes says how many bytes that is; *_out are HOST.
- * codes are 16-byte and scales 4-byte aligned (else RNNT_ERR_SHAPE, as are
- * negative counts; more than 2^31 - 1 rows or columns: RNNT_ERR_UNSUPPORTED).
+ * Both are 16-byte aligned (else RNNT_ERR_SHAPE, as are negative counts; more than
+ * 2^31 - 1 rows or columns: RNNT_ERR_UNSUPPORTED).
  */
 #define RNNT_MX4_BLOCK 32
 int rnnt_mx4_sizes(int64_t rows, int64_t cols, int64_t *codes_bytes_out, int64_t *scales_bytes_out);

@@ -3,12 +3,14 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "engine.h"
-#include "parts.h"
 
 namespace rnnt {
 
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
@@ -188,49 +190,236 @@ mx4_quantize_kernel(const void *x, long long rows, long long cols, long long str
         *reinterpret_cast<unsigned *>(scales + ((long long)rt * scale_tiles + st) * kScaleBytes + lane * 4) = *reinterpret_cast<const unsigned *>(tile + 4 * kTileBytes + lane * 4);
 }
 
-__device__ __forceinline__ void store(void *y, int type, long long at, float v)
+// Four neighbours of a row of y, rounded to its type; the first `left` of them
+__device__ __forceinline__ void store_four(void *y, int type, long long at, const float (&v)[4], long long left)
 {
-    if (type == RNNT_TYPE_F32) static_cast<float *>(y)[at] = v;
-    else if (type == RNNT_TYPE_BF16) static_cast<__bf16 *>(y)[at] = (__bf16)v;
-    else static_cast<_Float16 *>(y)[at] = (_Float16)v;
+    if (type == RNNT_TYPE_F32) store_piece<float, 4>(static_cast<float *>(y) + at, Piece<float, 4>{{v[0], v[1], v[2], v[3]}}, left);
+    else if (type == RNNT_TYPE_BF16) store_piece<__bf16, 4>(static_cast<__bf16 *>(y) + at, Piece<__bf16, 4>{{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]}}, left);
+    else store_piece<_Float16, 4>(static_cast<_Float16 *>(y) + at, Piece<_Float16, 4>{{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]}}, left);
 }
 
-// A wave computes 16 x 16 outputs: rows of w are the instruction's rows, rows of a its columns.
-template <int A>
+struct ProductArgs {
+    const void *a;
+    const unsigned char *a_scales, *w, *w_scales;
+    const float *bias;
+    void *y;
+    long long a_stride, y_stride;
+    int y_type, M, N, K;
+};
+
+__device__ __forceinline__ v8i operand(const v4u &c) { return v8i{(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0}; }
+
+// Few rows: latency bound.  A work-group computes 16 rows of a by 16 NT rows of w; its four waves take every fourth tile
+// of K each and add up at the end.  Operands go from memory to registers: a lane's part of a tile is a row's block, 32 values,
+// which it quantises by itself.
+template <int A, int NT>
 __global__ void __launch_bounds__(256)
-mx4_product_kernel(const void *a, const unsigned char *a_scales, long long a_stride, const unsigned char *w, const unsigned char *w_scales,
-                   const float *bias, void *y, int y_type, long long y_stride, long long M, long long N, long long K)
+mx4_product_kernel(const ProductArgs g)
 {
-    const int lane = threadIdx.x & 63, r = lane & 15, b = lane >> 4;
-    const long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const long long mts = tiles(M, kTileRows), nt = i / mts, mt = i - nt * mts;
-    if (nt >= tiles(N, kTileRows)) return;
-    const int steps = (int)tiles(K, kTileCols), scale_tiles = (int)tiles(K, kScaleCols);
-    v4f sum = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < steps; ++s) {
-        const v4u wc = *reinterpret_cast<const v4u *>(w + (nt * steps + s) * kTileBytes + lane * 16);
-        const unsigned ws = w_scales[(nt * scale_tiles + s / 4) * kScaleBytes + lane * 4 + (s & 3)];
-        v4u ac;
-        unsigned as;
+    constexpr int PITCH = NT * 16 + 4;
+    __shared__ __align__(16) float sums[4][16 * PITCH];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r = lane & 15, b = lane >> 4;
+    const int steps = (int)tiles(g.K, kTileCols), groups = (int)tiles(g.K, kScaleCols), n_tiles = (int)tiles(g.N, kTileRows);
+    const int across = (int)tiles(n_tiles, NT), mt = blockIdx.x / across, nt = (blockIdx.x - mt * across) * NT;
+    const long long row = (long long)mt * kTileRows + r;
+    v4f sum[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) sum[i] = v4f{0.f, 0.f, 0.f, 0.f};
+    for (int s = wave; s < steps; s += 4) {
+        v4u wc[NT], ac;
+        unsigned ws[NT], as;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const long long t = min(nt + i, n_tiles - 1);
+            wc[i] = *reinterpret_cast<const v4u *>(g.w + (t * steps + s) * kTileBytes + lane * 16);
+            ws[i] = g.w_scales[(t * groups + s / 4) * kScaleBytes + lane * 4 + (s & 3)];
+        }
         if constexpr (A == RNNT_TYPE_MX4) {
-            ac = *reinterpret_cast<const v4u *>(static_cast<const unsigned char *>(a) + (mt * steps + s) * kTileBytes + lane * 16);
-            as = a_scales[(mt * scale_tiles + s / 4) * kScaleBytes + lane * 4 + (s & 3)];
+            ac = *reinterpret_cast<const v4u *>(static_cast<const unsigned char *>(g.a) + ((long long)mt * steps + s) * kTileBytes + lane * 16);
+            as = g.a_scales[((long long)mt * groups + s / 4) * kScaleBytes + lane * 4 + (s & 3)];
         } else {
-            float v[32];
             typedef typename Element<A>::T T;
-            const long long row = mt * kTileRows + r, col = (long long)s * kTileCols + b * RNNT_MX4_BLOCK;
-            load_block<T>(v, static_cast<const T *>(a) + row * a_stride + col, row < M ? K - col : 0);
+            float v[32];
+            const int col = s * kTileCols + b * RNNT_MX4_BLOCK;
+            load_block<T>(v, static_cast<const T *>(g.a) + row * g.a_stride + col, row < g.M ? g.K - col : 0);
             ac = quantize_block(v, as);
         }
-        const v8i wv = {(int)wc.x, (int)wc.y, (int)wc.z, (int)wc.w, 0, 0, 0, 0}, av = {(int)ac.x, (int)ac.y, (int)ac.z, (int)ac.w, 0, 0, 0, 0};
-        sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, av, sum, 4, 4, 0, (int)ws, 0, (int)as);
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+            sum[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(wc[i]), operand(ac), sum[i], 4, 4, 0, (int)ws[i], 0, (int)as);
     }
-    const long long m = mt * kTileRows + r;
-    if (m >= M) return;
+    // (a lane holds four neighbours of w's rows for one of a's)
+#pragma unroll
+    for (int i = 0; i < NT; ++i) *reinterpret_cast<v4f *>(&sums[wave][r * PITCH + i * 16 + b * 4]) = sum[i];
+    __syncthreads();
+    const int m = threadIdx.x / (NT * 4), c = threadIdx.x % (NT * 4) * 4;
+    if (m >= 16 || (long long)mt * kTileRows + m >= g.M) return;
+    const long long n = (long long)nt * kTileRows + c;
+    if (n >= g.N) return;
+    float o[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const long long n = nt * kTileRows + b * 4 + e;
-        if (n < N) store(y, y_type, m * y_stride + n, sum[e] + (bias ? bias[n] : 0.f));
+        const int at = m * PITCH + c + e;
+        o[e] = ((sums[0][at] + sums[1][at]) + (sums[2][at] + sums[3][at])) + (g.bias && n + e < g.N ? g.bias[n + e] : 0.f);
+    }
+    store_four(g.y, g.y_type, ((long long)mt * kTileRows + m) * g.y_stride + n, o, g.N - n);
+}
+
+__device__ __forceinline__ const unsigned char *uniform(const unsigned char *p)
+{
+    const unsigned long long u = reinterpret_cast<unsigned long long>(p);
+    const unsigned lo = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)u), hi = (unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32));
+    return reinterpret_cast<const unsigned char *>((unsigned long long)hi << 32 | lo);
+}
+
+// Many rows: bound by the matrix instructions, 32 cycles for 32 x 32 x 64.  A work-group is 2 x 2 waves of TN x TM tiles
+// of 32 x 32 outputs (rows of w by rows of a).  Tiles of codes lie in memory as the lanes take them: they go to LDS in pieces of
+// 1 KB, four tiles of K in turn (STAGES), and from there to registers without bank conflicts.
+//
+// In a step (a tile of K, two instructions deep) the operands of the second half are read while the first half is
+// multiplied; then the wave waits for the next step's pieces, of which a step's time has passed since they were asked for, meets the others,
+// asks for the pieces three steps ahead (their place was last read a step ago), and reads the next step's first half while the second is
+// multiplied.  Scales: four steps' in a word, in LDS twice, asked for with the first step's codes.
+template <int TM, int TN>
+struct TileShape {
+    static constexpr int BM = TM * 64, BN = TN * 64, TILES = (BM + BN) / kTileRows, STAGES = 4;
+    static constexpr int CODES = TILES * kTileBytes, SCALES = TILES * kScaleBytes, LDS = STAGES * CODES + 2 * SCALES;
+};
+
+template <int TM, int TN>
+__global__ void __launch_bounds__(256)
+mx4_tile_kernel(const ProductArgs g, int m_blocks, int n_blocks)
+{
+    typedef TileShape<TM, TN> S;
+    constexpr int LOADS = S::TILES / 4, SCALE_LOADS = S::TILES / 16;       // of a wave: a tile of codes each, four tiles' scales each
+    static_assert(S::TILES % 16 == 0, "whole loads for four waves");
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int steps = (int)tiles(g.K, kTileCols), groups = (int)tiles(g.K, kScaleCols);
+    // Blocks of an XCD follow each other, in bands of eight blocks of rows of a, so that its L2 serves each operand to several.
+    int mb, nb;
+    {
+        const int n = m_blocks * n_blocks, xcd = blockIdx.x & 7, at = xcd * (n / 8) + min(xcd, n % 8) + (blockIdx.x >> 3);
+        const int band = at / (8 * n_blocks), in = at - band * 8 * n_blocks, high = min(8, m_blocks - band * 8);
+        nb = in / high;
+        mb = band * 8 + in - nb * high;
+    }
+    const int m_last = (int)tiles(g.M, kTileRows) - 1, n_last = (int)tiles(g.N, kTileRows) - 1;
+    // row of tiles number i of the block: first those of a, then those of w; what is beyond the end repeats the last one and is not stored
+    auto tile_row = [&](int i) { return i < S::BM / 16 ? min(mb * (S::BM / 16) + i, m_last) : min(nb * (S::BN / 16) + i - S::BM / 16, n_last); };
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds;
+    const unsigned char *code[LOADS], *scale[SCALE_LOADS];
+    unsigned scale_off[SCALE_LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int t = wave * LOADS + i;
+        code[i] = uniform((t < S::BM / 16 ? static_cast<const unsigned char *>(g.a) : g.w) + (long long)tile_row(t) * steps * kTileBytes);
+    }
+#pragma unroll
+    for (int i = 0; i < SCALE_LOADS; ++i) {
+        // (four rows of tiles of one operand: their first one's address, and a lane's distance from it)
+        const int t = (wave * SCALE_LOADS + i) * 4, first = tile_row(t);
+        scale[i] = uniform((t < S::BM / 16 ? g.a_scales : g.w_scales) + (long long)first * groups * kScaleBytes);
+        scale_off[i] = (unsigned)(tile_row(t + (lane >> 4)) - first) * (unsigned)groups * kScaleBytes + (lane & 15) * 16;
+    }
+    auto to_lds = [&](const unsigned char *from, unsigned off, unsigned to) {
+        const unsigned m = (unsigned)__builtin_amdgcn_readfirstlane((int)(lds0 + to));
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" :: "v"(off), "s"(m), "s"(from) : "memory");
+    };
+    // pieces of step s (beyond the end those of the last one again, so that every step has as many) to stage `at`
+    auto ask = [&](int s, int at, bool with_scales) {
+        const long long k = min(s, steps - 1);
+        if (with_scales) {
+#pragma unroll
+            for (int i = 0; i < SCALE_LOADS; ++i)
+                to_lds(uniform(scale[i] + k / 4 * kScaleBytes), scale_off[i], (unsigned)(S::STAGES * S::CODES + (s / 4 & 1) * S::SCALES + (wave * SCALE_LOADS + i) * 1024));
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) to_lds(uniform(code[i] + k * kTileBytes), (unsigned)lane * 16u, (unsigned)(at * S::CODES + (wave * LOADS + i) * kTileBytes));
+    };
+    const int wm = wave & 1, wn = wave >> 1;
+    // a lane's operand of 32 rows and half h of a tile: rows lane % 32, block 2 h + lane / 32
+    const unsigned char *mine = lds + (lane >> 4 & 1) * kTileBytes + (lane >> 5) * 256 + (lane & 15) * 16;
+    auto read = [&](int stage, int tile, int h) { return *reinterpret_cast<const v4u *>(mine + stage * S::CODES + tile * kTileBytes + h * 512); };
+    const unsigned char *mine_s = lds + S::STAGES * S::CODES + (lane >> 4 & 1) * kScaleBytes + (lane >> 5) * 64 + (lane & 15) * 4;
+    auto read_scale = [&](int group, int tile, int h) { return *reinterpret_cast<const int *>(mine_s + (group & 1) * S::SCALES + tile * kScaleBytes + h * 128); };
+    struct Half { v4u a[TM], w[TN]; };
+    struct Scales { int a[2][TM], w[2][TN]; };
+    auto read_half = [&](Half &o, int stage, int h) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) o.a[i] = read(stage, wm * TM * 2 + i * 2, h);
+#pragma unroll
+        for (int i = 0; i < TN; ++i) o.w[i] = read(stage, S::BM / 16 + wn * TN * 2 + i * 2, h);
+    };
+    auto read_scales = [&](Scales &o, int group) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) o.a[h][i] = read_scale(group, wm * TM * 2 + i * 2, h);
+#pragma unroll
+            for (int i = 0; i < TN; ++i) o.w[h][i] = read_scale(group, S::BM / 16 + wn * TN * 2 + i * 2, h);
+        }
+    };
+    v16f sum[TN][TM];
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum[i][j][e] = 0.f;
+    if (steps > 0) {
+        Half half[2];
+        Scales now, next;
+        ask(0, 0, true);
+        ask(1, 1, false);
+        ask(2, 2, false);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(2 * LOADS) : "memory");
+        read_scales(now, 0);
+        read_half(half[0], 0, 0);
+        auto step = [&](int t, auto number) {
+            constexpr int I = decltype(number)::value;     // t % 4
+            read_half(half[1], I, 1);
+#pragma unroll
+            for (int i = 0; i < TN; ++i)
+#pragma unroll
+                for (int j = 0; j < TM; ++j)
+                    sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(half[0].w[i]), operand(half[0].a[j]), sum[i][j], 4, 4, I, now.w[0][i], I, now.a[0][j]);
+            // what step t + 1 needs is there; of step t + 2 it may still be on its way
+            asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(LOADS + (I == 2 ? SCALE_LOADS : 0)) : "memory");
+            ask(t + 3, (I + 3) % 4, I == 1);
+            if constexpr (I == 3) read_scales(next, t / 4 + 1);
+            read_half(half[0], (I + 1) % 4, 0);
+#pragma unroll
+            for (int i = 0; i < TN; ++i)
+#pragma unroll
+                for (int j = 0; j < TM; ++j)
+                    sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(half[1].w[i]), operand(half[1].a[j]), sum[i][j], 4, 4, I, now.w[1][i], I, now.a[1][j]);
+            if constexpr (I == 3) now = next;
+        };
+        for (int t = 0; t < steps; t += 4) {
+            step(t, std::integral_constant<int, 0>());
+            if (t + 1 < steps) step(t + 1, std::integral_constant<int, 1>());
+            if (t + 2 < steps) step(t + 2, std::integral_constant<int, 2>());
+            if (t + 3 < steps) step(t + 3, std::integral_constant<int, 3>());
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing is on its way to LDS that is given up)
+    }
+    // Register v of lane l holds row 8 (v / 4) + 4 (l / 32) + v % 4 of w's 32, row l % 32 of a's.
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+        const long long m = (long long)mb * S::BM + wm * TM * 32 + j * 32 + (lane & 31);
+        if (m >= g.M) continue;
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const long long n = (long long)nb * S::BN + wn * TN * 32 + i * 32 + q * 8 + (lane >> 5) * 4;
+                if (n >= g.N) continue;
+                float o[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = sum[i][j][q * 4 + e] + (g.bias && n + e < g.N ? g.bias[n + e] : 0.f);
+                store_four(g.y, g.y_type, m * g.y_stride + n, o, g.N - n);
+            }
     }
 }
 
@@ -251,6 +440,16 @@ constexpr int64_t kMost = 0x7fffffff;
 bool is_number(int32_t type) { return type == RNNT_TYPE_F32 || type == RNNT_TYPE_BF16 || type == RNNT_TYPE_F16; }
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 uintptr_t size_of(int32_t type) { return type == RNNT_TYPE_F32 ? 4 : 2; }
+
+// Which kernel computes a product
+enum Plan { kDirect, kTiles128, kTiles256 };
+constexpr int64_t kDirectGroups = 256, kDirectRows = 512;
+int64_t direct_groups(int64_t M, int64_t N, int nt) { return tiles(M, kTileRows) * tiles(tiles(N, kTileRows), nt); }
+Plan plan_of(int64_t M, int64_t N, int64_t K)
+{
+    if (M <= kDirectRows || K == 0) return kDirect;
+    return tiles(M, 256) * tiles(N, 256) >= 256 ? kTiles256 : kTiles128;
+}
 
 }  // namespace
 
@@ -273,7 +472,7 @@ int rnnt_mx4_quantize(const void *x, int32_t type, int64_t rows, int64_t cols, i
     if (rows > kMost || cols > kMost) return RNNT_ERR_UNSUPPORTED;
     if (rows == 0 || cols == 0) return RNNT_OK;
     if (!x || !codes_out || !scales_out) return RNNT_ERR_NULL;
-    if (!aligned(x, size_of(type)) || !aligned(codes_out, 16) || !aligned(scales_out, 4) || !aligned(values_out, 4)) return RNNT_ERR_SHAPE;
+    if (!aligned(x, size_of(type)) || !aligned(codes_out, 16) || !aligned(scales_out, 16) || !aligned(values_out, 4)) return RNNT_ERR_SHAPE;
     const int ct = (int)tiles(cols, kTileCols), st = (int)tiles(cols, kScaleCols);
     const long long blocks = tiles(rows, kTileRows) * st;
     if (blocks > kMost) return RNNT_ERR_UNSUPPORTED;
@@ -293,7 +492,9 @@ int rnnt_mx4_product_workspace(int32_t a_type, int64_t M, int64_t N, int64_t K, 
     if (!bytes_out) return RNNT_ERR_NULL;
     if ((!is_number(a_type) && a_type != RNNT_TYPE_MX4) || M < 0 || N < 0 || K < 0) return RNNT_ERR_SHAPE;
     if (M > kMost || N > kMost || K > kMost) return RNNT_ERR_UNSUPPORTED;
-    *bytes_out = 0;
+    int64_t codes = 0, scales = 0;
+    if (a_type != RNNT_TYPE_MX4 && plan_of(M, N, K) != kDirect) (void)rnnt_mx4_sizes(M, K, &codes, &scales);
+    *bytes_out = codes + scales;
     return RNNT_OK;
 }
 
@@ -308,22 +509,47 @@ int rnnt_mx4_product(const void *a, const void *a_scales, int32_t a_type, int64_
     if (!is_number(y_type) || y_stride < N || (!codes && a_stride < K) || workspace_bytes < 0) return RNNT_ERR_SHAPE;
     if (M == 0 || N == 0) return RNNT_OK;
     if (!y || (K > 0 && (!a || (codes && !a_scales) || !w_codes || !w_scales))) return RNNT_ERR_NULL;
-    if (!aligned(y, size_of(y_type)) || !aligned(bias, 4) || !aligned(w_codes, 16) || !aligned(w_scales, 4) ||
-        !aligned(a, codes ? 16 : size_of(a_type)) || (codes && !aligned(a_scales, 4))) return RNNT_ERR_SHAPE;
+    if (!aligned(y, size_of(y_type)) || !aligned(bias, 4) || !aligned(w_codes, 16) || !aligned(w_scales, 16) ||
+        !aligned(a, codes ? 16 : size_of(a_type)) || (codes && !aligned(a_scales, 16))) return RNNT_ERR_SHAPE;
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return RNNT_ERR_SCRATCH;
-    const long long blocks = tiles(tiles(M, kTileRows) * tiles(N, kTileRows), 4);
-    if (blocks > kMost) return RNNT_ERR_UNSUPPORTED;
-    auto run = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, static_cast<hipStream_t>(stream), a, static_cast<const unsigned char *>(a_scales),
-                           (long long)a_stride, static_cast<const unsigned char *>(w_codes), static_cast<const unsigned char *>(w_scales), bias, y,
-                           (int)y_type, (long long)y_stride, (long long)M, (long long)N, (long long)K);
+    const hipStream_t on = static_cast<hipStream_t>(stream);
+    ProductArgs args{a, static_cast<const unsigned char *>(a_scales), static_cast<const unsigned char *>(w_codes), static_cast<const unsigned char *>(w_scales),
+                     bias, y, a_stride, y_stride, y_type, (int)M, (int)N, (int)K};
+    const Plan plan = plan_of(M, N, K);
+    if (plan == kDirect) {
+        const int nt = direct_groups(M, N, 4) >= kDirectGroups ? 4 : 1;
+        const int64_t blocks = direct_groups(M, N, nt);
+        if (blocks > kMost) return RNNT_ERR_UNSUPPORTED;
+        auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, on, args); };
+        auto with = [&](auto type) {
+            constexpr int A = decltype(type)::value;
+            if (nt == 4) run(mx4_product_kernel<A, 4>); else run(mx4_product_kernel<A, 1>);
+        };
+        if (a_type == RNNT_TYPE_F32) with(std::integral_constant<int, RNNT_TYPE_F32>());
+        else if (a_type == RNNT_TYPE_BF16) with(std::integral_constant<int, RNNT_TYPE_BF16>());
+        else if (a_type == RNNT_TYPE_F16) with(std::integral_constant<int, RNNT_TYPE_F16>());
+        else with(std::integral_constant<int, RNNT_TYPE_MX4>());
+        MX4_TRY(hipGetLastError());
+        return RNNT_OK;
+    }
+    if (!codes) {
+        int64_t cb = 0, sb = 0;
+        (void)rnnt_mx4_sizes(M, K, &cb, &sb);
+        unsigned char *to = static_cast<unsigned char *>(workspace);
+        if (const int rc = rnnt_mx4_quantize(a, a_type, M, K, a_stride, to, to + cb, nullptr, stream)) return rc;
+        args.a = to;
+        args.a_scales = to + cb;
+    }
+    auto run = [&](auto kernel, int bm, int bn, unsigned lds) -> int {
+        const int64_t mb = tiles(M, bm), nb = tiles(N, bn);
+        if (mb * nb > kMost / 8) return RNNT_ERR_UNSUPPORTED;
+        MX4_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(mb * nb)), dim3(256), lds, on, args, (int)mb, (int)nb);
+        MX4_TRY(hipGetLastError());
+        return RNNT_OK;
     };
-    if (a_type == RNNT_TYPE_F32) run(mx4_product_kernel<RNNT_TYPE_F32>);
-    else if (a_type == RNNT_TYPE_BF16) run(mx4_product_kernel<RNNT_TYPE_BF16>);
-    else if (a_type == RNNT_TYPE_F16) run(mx4_product_kernel<RNNT_TYPE_F16>);
-    else run(mx4_product_kernel<RNNT_TYPE_MX4>);
-    MX4_TRY(hipGetLastError());
-    return RNNT_OK;
+    if (plan == kTiles256) return run(mx4_tile_kernel<4, 4>, 256, 256, TileShape<4, 4>::LDS);
+    return run(mx4_tile_kernel<2, 2>, 128, 128, TileShape<2, 2>::LDS);
 }
 
 }  // extern "C"

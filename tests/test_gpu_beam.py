@@ -192,6 +192,22 @@ def test_states_follow_the_hypotheses(pkg, B, k_in, k_out, row):  # noqa: F811
             assert np.array_equal(d.cpu().numpy(), _reorder(s, parents, k_in))
 
 
+def test_large_states(pkg):  # noqa: F811
+    """More than the L2s hold, out of place and within themselves, in rows of whole and of broken 16 bytes."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for row, dtype in ((40000, torch.float32), (40001, torch.bfloat16)):
+        src = torch.randn((2, 32, 8, row), generator=g, device="cuda").to(dtype)
+        parents = torch.randint(-1, 8, (32, 8), generator=g, device="cuda", dtype=torch.int32)
+        dst = torch.full_like(src, 5)
+        pkg.beam_reorder([(src, dst)], parents)
+        at = parents.clamp(min=0).long()
+        want = src[:, torch.arange(32, device="cuda")[:, None], at] * (parents >= 0)[..., None]
+        assert torch.equal(dst, want)
+        pkg.beam_reorder([(src, src)], parents)
+        assert torch.equal(src, want)
+
+
 def test_states_with_strides_of_their_own(pkg):  # noqa: F811
     """Hidden and cell vectors in one buffer, double buffers side by side, one source for all utterances."""
     import torch

@@ -116,6 +116,10 @@ SHAPES = [(1, 1, 1), (1, 17, 32), (3, 5, 33), (8, 1025, 640), (16, 16, 128), (17
 @pytest.mark.parametrize("M,N,K", SHAPES)
 @pytest.mark.parametrize("a_type,y_type", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("mx4", "f32"), ("mx4", "bf16"), ("bf16", "f32")])
 def test_products(pkg, M, N, K, a_type, y_type):  # noqa: F811
+    _products(pkg, M, N, K, a_type, y_type)
+
+
+def _products(pkg, M, N, K, a_type, y_type):  # noqa: F811
     import torch
     g = torch.Generator().manual_seed(M + 3 * N + 5 * K)
     a = torch.randn((M, K), generator=g) * torch.exp2(torch.randint(-3, 4, (M, 1), generator=g).float())
@@ -141,6 +145,13 @@ def test_products(pkg, M, N, K, a_type, y_type):  # noqa: F811
     ws = torch.full((need + 16,), 0xFF, dtype=torch.uint8, device="cuda")
     again = wm.product(am, bias=None if bias is None else bias.cuda(), dtype=_torch_type(y_type), workspace=ws)
     assert torch.equal(again, got)
+
+
+@pytest.mark.parametrize("M,N,K", [(4099, 4100, 300), (8200, 2050, 1290), (4000, 8000, 128)])
+@pytest.mark.parametrize("a_type,y_type", [("mx4", "f32"), ("bf16", "bf16")])
+def test_large_products(pkg, M, N, K, a_type, y_type):  # noqa: F811
+    """Sizes that the largest tiles are chosen for, with rows and columns that end inside one."""
+    _products(pkg, M, N, K, a_type, y_type)
 
 
 @pytest.mark.parametrize("M", [5, 300, 2050])

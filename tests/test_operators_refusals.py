@@ -32,7 +32,7 @@ def test_quantize(lib):
     assert f(rows=0) == OK and f(cols=0, stride=0) == OK and f(rows=0, x=None, codes=None) == OK
     assert f(x=None) == NULL and f(codes=None) == NULL and f(scales=None) == NULL
     assert f(type=3) == SHAPE and f(type=-1) == SHAPE and f(rows=-1) == SHAPE and f(cols=-1) == SHAPE and f(stride=63) == SHAPE
-    assert f(x=P + 2) == SHAPE and f(x=P + 1, type=1) == SHAPE and f(codes=P + 8) == SHAPE and f(scales=P + 2) == SHAPE and f(values=P + 1) == SHAPE
+    assert f(x=P + 2) == SHAPE and f(x=P + 1, type=1) == SHAPE and f(codes=P + 8) == SHAPE and f(scales=P + 4) == SHAPE and f(values=P + 1) == SHAPE
     assert f(rows=2 ** 31) == UNSUPPORTED
 
 
@@ -43,7 +43,7 @@ def test_product(lib):
     assert f(a=None) == NULL and f(a_scales=None) == NULL and f(w=None) == NULL and f(ws=None) == NULL and f(y=None) == NULL
     assert f(a_type=4) == SHAPE and f(y_type=3) == SHAPE and f(y_stride=63) == SHAPE and f(M=-1) == SHAPE and f(N=-1) == SHAPE and f(K=-1) == SHAPE
     assert f(a_type=0, a_stride=127) == SHAPE and f(space_bytes=-1) == SHAPE
-    assert f(a=P + 8) == SHAPE and f(a_scales=P + 1) == SHAPE and f(w=P + 4) == SHAPE and f(ws=P + 2) == SHAPE and f(bias=P + 2) == SHAPE
+    assert f(a=P + 8) == SHAPE and f(a_scales=P + 4) == SHAPE and f(w=P + 4) == SHAPE and f(ws=P + 8) == SHAPE and f(bias=P + 2) == SHAPE
     assert f(y=P + 2) == SHAPE and f(y=P + 1, y_type=1) == SHAPE and f(a=P + 2, a_type=0, a_stride=128) == SHAPE
     assert f(M=2 ** 31) == UNSUPPORTED and f(K=2 ** 31) == UNSUPPORTED
     need = ctypes.c_int64(-1)
