@@ -12,8 +12,7 @@
 namespace rnnt {
 
 constexpr int kMaxBeams = 64;
-constexpr int kTile = 1024;             // values of a row that a wave looks at together, 16 a lane
-constexpr int kPerLane = kTile / 64;
+constexpr int kTile = 1024;             // logits of a row that a wave looks at together, 16 a lane
 constexpr int kBuffer = 128;            // candidates of a wave that wait to be sorted in
 constexpr int kJoinWaves = 16;          // waves of a work-group that joins lists, at most
 
@@ -30,7 +29,7 @@ struct SelectArgs {
     int pieces, piece_tiles;            // a row is cut into so many pieces of so many tiles
     u64 *lists;                         // [B][beams][pieces][n_out]: the pieces' best,
     double *sums;                       // [B][beams][pieces]: sums of exponentials
-    float *tops;                        // and the logit that those are relative to (in the workspace; of one launch: in LDS)
+    float *tops;                        // and the logit that those are relative to
 };
 
 // The value of lane ^ M
@@ -126,19 +125,35 @@ template <> struct Logit<RNNT_TYPE_F32> { typedef float T; };
 template <> struct Logit<RNNT_TYPE_BF16> { typedef __bf16 T; };
 template <> struct Logit<RNNT_TYPE_F16> { typedef _Float16 T; };
 
-// One pass over a piece of a row: the running maximum and sum of a softmax, a lane's own, and the best n of its logits.
-// A logit that is not above the n-th best so far goes by at the price of a comparison for a lane's 16; the others
-// are put into a buffer, which is sorted and joined with the list 64 at a time.  Before there is a list, the maxima of n or more
-// groups of lanes bound the n-th best from below.
+// Wave-wide maximum and sum
+__device__ __forceinline__ float wave_max(float v)
+{
+    v = fmaxf(v, from_lane<1>(v)); v = fmaxf(v, from_lane<2>(v)); v = fmaxf(v, from_lane<4>(v));
+    v = fmaxf(v, from_lane<8>(v)); v = fmaxf(v, from_lane<16>(v)); return fmaxf(v, from_lane<32>(v));
+}
+__device__ __forceinline__ double wave_sum(double v)
+{
+    v += from_lane<1>(v); v += from_lane<2>(v); v += from_lane<4>(v);
+    v += from_lane<8>(v); v += from_lane<16>(v); return v + from_lane<32>(v);
+}
+
+constexpr float kLog2E = 1.44269504f, kLowest = -3.402823466e38f;
+
+// One pass over a piece of a row by a wave: the running maximum and sum of a softmax, a lane's own, and the best n of its
+// logits.  A tile is 16 logits a lane (and 64 more where the row ends with them: vocabularies are a power of two and a blank).
+// A tile none of whose logits is above the n-th best so far goes by at the price of one comparison; of the others a lane
+// notes which of its own are, and one a lane at a time they go into a buffer, which is sorted and joined with the list 64 at a time.
+// Before there is a list, the maxima of n or more groups of lanes bound the n-th best from below.
 template <class T> struct Scan {
-    static constexpr int PER = 16 / sizeof(T), LOADS = kPerLane / PER;
+    static constexpr int PER = 16 / sizeof(T), LOADS = kTile / 64 / PER, ALL = kTile / 64 + 1;
     struct __attribute__((packed, aligned(sizeof(T)))) At { T e[PER]; };
     const T *row;
     u64 *buffer;
     int n, lane;
     int count = 0;                 // in the buffer
+    bool started = false;          // there is a list
     float bar = -INFINITY;         // logits above it are looked at
-    float top = -3.402823466e38f;  // (never -inf: differences to it are numbers)
+    float top = kLowest;           // (never -inf: differences to it are numbers)
     double sum = 0;
     InRow list{0};
 
@@ -151,16 +166,11 @@ template <class T> struct Scan {
         buffer[lane] = rest;
         count = max(count - 64, 0);
         sort_wave<true>(v);
-        join(list, v);
+        if (started) join(list, v);
+        else list = reverse(v);
+        started = true;
         const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(list.key >> 32), n - 1);
         if (hi != 0u) bar = key_logit((u64)hi << 32);
-    }
-    __device__ __forceinline__ void append(float x, int token)
-    {
-        const bool in = x > bar;
-        const u64 all = __ballot(in);
-        if (in) buffer[count + __builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0u))] = row_key(x, token);
-        count += __popcll(all);
     }
     __device__ __forceinline__ void first_bar(float m)
     {
@@ -176,184 +186,149 @@ template <class T> struct Scan {
         const unsigned u = __float_as_uint(t);
         bar = t == -INFINITY ? t : __uint_as_float(t == 0.f ? 0x80000001u : t > 0.f ? u - 1u : u + 1u);
     }
-    // token(i): where f[i] stands; again(j): the logits from base + j * 64 on, one a lane, for more candidates than the buffer takes
-    template <class Token>
-    __device__ __forceinline__ void take(const float (&f)[kPerLane], int base, int end, bool first, Token token)
+    At next[LOADS];
+    T more;
+    __device__ __forceinline__ void load(int base, int to)
     {
-        float m = f[0];
 #pragma unroll
-        for (int i = 1; i < kPerLane; ++i) m = fmaxf(m, f[i]);
-        constexpr float kLog2E = 1.44269504f;
-        const float next = fmaxf(top, m);
-        float part = 0.f;
-#pragma unroll
-        for (int i = 0; i < kPerLane; ++i) part += __builtin_amdgcn_exp2f((f[i] - next) * kLog2E);
-        sum = sum * (double)__builtin_amdgcn_exp2f((top - next) * kLog2E) + (double)part;
-        top = next;
-        if (first) first_bar(m);
-        if (__ballot(m > bar) == 0ull) return;
-        int more = 0;
-#pragma unroll
-        for (int i = 0; i < kPerLane; ++i) more += __popcll(__ballot(f[i] > bar));
-        if (count + more <= kBuffer) {
-#pragma unroll
-            for (int i = 0; i < kPerLane; ++i) append(f[i], token(i));
-            if (count >= 64) flush();
-            if (count >= 64) flush();
-        } else {
-            for (int j = lane; j - lane < end - base; j += 64) {
-                append(j < end - base ? (float)row[base + j] : -INFINITY, base + j);
-                if (count >= 64) flush();
-            }
-        }
+        for (int q = 0; q < LOADS; ++q) next[q] = *reinterpret_cast<const At *>(row + base + (q * 64 + lane) * PER);
+        more = row[base + min(kTile + lane, to - 1 - base)];
     }
+    __device__ __forceinline__ void begin(int from, int to) { if (to - from >= kTile) load(from, to); }
+    // (tokens may go on to the largest int)
     __device__ __forceinline__ void run(int from, int to)
     {
-        At next[LOADS];
-        auto load = [&](int base) {
+        for (int base = from; base < to;) {
+            const int rest = to - base, size = rest <= kTile + 64 ? rest : kTile;
+            const bool full = rest >= kTile;
+            float f[ALL];
+            if (full) {
 #pragma unroll
-            for (int q = 0; q < LOADS; ++q) next[q] = *reinterpret_cast<const At *>(row + base + (q * 64 + lane) * PER);
-        };
-        int base = from;                                   // (tokens may go on to the largest int)
-        if (to - base >= kTile) load(base);
-        for (; to - base >= kTile; base += kTile) {
-            float f[kPerLane];
+                for (int i = 0; i < ALL - 1; ++i) f[i] = (float)next[i / PER].e[i % PER];
+                f[ALL - 1] = kTile + lane < size ? (float)more : -INFINITY;
+                if (rest - size >= kTile) load(base + size, to);
+            } else {
+                T v[ALL - 1];
 #pragma unroll
-            for (int i = 0; i < kPerLane; ++i) f[i] = (float)next[i / PER].e[i % PER];
-            if (to - base >= 2 * kTile) load(base + kTile);
-            take(f, base, base + kTile, base == from, [&](int i) { return base + (i / PER * 64 + lane) * PER + i % PER; });
-        }
-        if (base < to) {
-            float f[kPerLane];
+                for (int i = 0; i < ALL - 1; ++i) v[i] = row[base + min(i * 64 + lane, rest - 1)];
 #pragma unroll
-            for (int i = 0; i < kPerLane; ++i) {
-                const int j = i * 64 + lane;
-                const float x = (float)row[base + min(j, to - base - 1)];
-                f[i] = j < to - base ? x : -INFINITY;
+                for (int i = 0; i < ALL - 1; ++i) f[i] = i * 64 + lane < rest ? (float)v[i] : -INFINITY;
+                f[ALL - 1] = -INFINITY;
             }
-            take(f, base, to, base == from, [&](int i) { return base + i * 64 + lane; });
+            float m = f[0];
+#pragma unroll
+            for (int i = 1; i < ALL; ++i) m = fmaxf(m, f[i]);
+            const float high = fmaxf(top, m);
+            float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < ALL; ++i) part[i % 4] += __builtin_amdgcn_exp2f((f[i] - high) * kLog2E);
+            sum = sum * (double)__builtin_amdgcn_exp2f((top - high) * kLog2E) + (double)((part[0] + part[1]) + (part[2] + part[3]));
+            top = high;
+            if (base == from) first_bar(m);
+            const bool last = size == rest;
+            unsigned mine = 0;                             // a lane's logits above the bar
+            if (__ballot(m > bar) != 0ull) {
+#pragma unroll
+                for (int i = 0; i < ALL; ++i) mine |= f[i] > bar ? 1u << i : 0u;
+            }
+            for (;;) {
+                const u64 any = __ballot(mine != 0u);
+                if (any != 0ull) {
+                    const int i = __builtin_ctz(mine | 0x80000000u);
+                    const int in_tile = !full ? i * 64 + lane : i < ALL - 1 ? (i / PER * 64 + lane) * PER + i % PER : kTile + lane;
+                    const float x = mine != 0u ? (float)row[base + in_tile] : -INFINITY;
+                    // (the bar may have risen to a logit with a higher token)
+                    const bool in = mine != 0u && x >= bar;
+                    const u64 all = __ballot(in);
+                    if (in) buffer[count + __builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0u))] = row_key(x, base + in_tile);
+                    count += __popcll(all);
+                    mine &= mine - 1u;
+                }
+                const bool end = any == 0ull;
+                if (count >= 64 || (end && last && count > 0)) flush();
+                if (end) break;
+            }
+            base += size;
         }
-        if (count > 0) flush();
-        // over the lanes
-        float all = top;
-        all = fmaxf(all, from_lane<1>(all)); all = fmaxf(all, from_lane<2>(all)); all = fmaxf(all, from_lane<4>(all));
-        all = fmaxf(all, from_lane<8>(all)); all = fmaxf(all, from_lane<16>(all)); all = fmaxf(all, from_lane<32>(all));
-        sum *= (double)__builtin_amdgcn_exp2f((top - all) * 1.44269504f);
-        sum += from_lane<1>(sum); sum += from_lane<2>(sum); sum += from_lane<4>(sum);
-        sum += from_lane<8>(sum); sum += from_lane<16>(sum); sum += from_lane<32>(sum);
+        const float all = wave_max(top);
+        sum = wave_sum(sum * (double)__builtin_amdgcn_exp2f((top - all) * kLog2E));
         top = all;
     }
 };
 
-// Piece `at` (of [B][beams][pieces]) by a wave; `slot`: where in the tables its results go
-template <int TYPE>
-__device__ __forceinline__ void scan_piece(const SelectArgs &a, long long at, u64 *buffer, u64 *lists, double *sums, float *tops, long long slot)
+// A hypothesis' row or a piece of it
+template <class T> __device__ __forceinline__ Scan<T> scan_of(const SelectArgs &a, int b, int k, u64 *buffer)
 {
-    typedef typename Logit<TYPE>::T T;
-    const long long hyp = at / a.pieces;
-    const int piece = (int)(at - hyp * a.pieces);
-    const long long b = hyp / a.beams;
-    const int k = (int)(hyp - b * a.beams);
-    const int lane = threadIdx.x & 63;
-    // (nothing of a finished hypothesis, or of one that does not exist, is looked at again)
-    if ((a.finished && a.finished[hyp]) || a.scores[hyp] == -INFINITY) return;
     Scan<T> s;
     s.row = static_cast<const T *>(a.logits) + b * a.batch_stride + k * a.beam_stride;
-    s.buffer = buffer; s.n = a.n_out; s.lane = lane;
-    const long long from = (long long)piece * a.piece_tiles * kTile;
-    s.run((int)from, (int)min(from + (long long)a.piece_tiles * kTile, (long long)a.V));
-    if (lane < a.n_out) lists[slot * a.n_out + lane] = s.list.key;
-    if (lane == 0) { sums[slot] = s.sum; tops[slot] = s.top; }
+    s.buffer = buffer; s.n = a.n_out; s.lane = threadIdx.x & 63;
+    return s;
 }
 
-// The lists of an utterance's rows become one, by the waves of a work-group: hypothesis by hypothesis with its scores, then
-// wave by wave.  tokens: [beams][n_out], tree: [waves][64] keys and as many words, in LDS.
-__device__ __forceinline__ void join_rows(const SelectArgs &a, int b, int waves, const u64 *lists, const double *sums, const float *tops,
-                                          int *tokens, u64 *tree_keys, unsigned *tree_from)
-{
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = a.n_out;
+// The waves of a work-group make one list of an utterance's rows: hypothesis by hypothesis with its score, then wave by wave.
+struct Joined {
+    const SelectArgs &a;
+    int *tokens;           // [beams][n_out], in LDS
+    int lane;
     InAll best{0, 0};
-    for (int k = wave; k < a.beams; k += waves) {
-        const long long hyp = (long long)b * a.beams + k;
-        const float score = a.scores[hyp];
-        InRow list{0};
-        double base = -INFINITY;
-        float top = 0.f;
-        if (a.finished && a.finished[hyp]) {
-            base = (double)score;
-            if (lane == 0) list.key = row_key(0.f, a.end_token);
-        } else if (score > -INFINITY) {
-            const u64 *mine = lists + (long long)k * a.pieces * n;
-            list.key = lane < n ? mine[lane] : 0;
-            for (int s = 1; s < a.pieces; ++s) join(list, InRow{63 - lane < n ? mine[s * n + 63 - lane] : 0});
-            // of the pieces' sums: a lane a piece
-            top = lane < a.pieces ? tops[k * a.pieces + lane] : -3.402823466e38f;
-            float all = top;
-            all = fmaxf(all, from_lane<1>(all)); all = fmaxf(all, from_lane<2>(all)); all = fmaxf(all, from_lane<4>(all));
-            all = fmaxf(all, from_lane<8>(all)); all = fmaxf(all, from_lane<16>(all)); all = fmaxf(all, from_lane<32>(all));
-            double sum = lane < a.pieces ? sums[k * a.pieces + lane] * exp((double)top - (double)all) : 0.0;
-            sum += from_lane<1>(sum); sum += from_lane<2>(sum); sum += from_lane<4>(sum);
-            sum += from_lane<8>(sum); sum += from_lane<16>(sum); sum += from_lane<32>(sum);
-            top = all;
-            base = (double)score - log(sum);               // (NaN where the row holds a NaN or an infinity)
-        }
-        InAll item{0, ~(unsigned)(k * 64 + lane)};
-        if (list.key != 0) {
-            const double t = base + ((double)key_logit(list.key) - (double)top) + 0.0;
-            const u64 u = __builtin_bit_cast(u64, t);
-            if (t > -INFINITY) item.key = u >> 63 ? ~u : u | 0x8000000000000000ull;
-        }
-        if (lane < n) tokens[k * n + lane] = (int)~(unsigned)list.key;
-        if (k == wave) best = item;
-        else join(best, reverse(item));
-    }
-    for (int half = waves / 2; half > 0; half /= 2) {
-        if (wave >= half && wave < 2 * half) { tree_keys[wave * 64 + lane] = best.key; tree_from[wave * 64 + lane] = best.from; }
-        __syncthreads();
-        if (wave < half) join(best, InAll{tree_keys[(wave + half) * 64 + 63 - lane], tree_from[(wave + half) * 64 + 63 - lane]});
-    }
-    __syncthreads();                                       // (one wave alone: its tokens)
-    if (wave == 0 && lane < n) {
-        const long long o = (long long)b * n + lane;
-        const int from = (int)~best.from, k = from >> 6;
-        const u64 u = best.key >> 63 ? best.key ^ 0x8000000000000000ull : ~best.key;
-        a.scores_out[o] = best.key ? (float)__builtin_bit_cast(double, u) : -INFINITY;
-        a.tokens_out[o] = best.key ? tokens[k * n + (from & 63)] : -1;
-        a.parents_out[o] = best.key ? k : -1;
-    }
-}
-
-// Where LDS goes in a launch that scans and joins
-struct SelectLds {
-    size_t buffers, tokens, lists, sums, tops, bytes;
-    __host__ __device__ SelectLds(int waves, int beams, int pieces, int n)
+    bool first = true;
+    // the best of hypothesis k; ended: its only candidate is the end token
+    __device__ __forceinline__ void add(int k, float score, bool ended, InRow list, float top, double sum)
     {
-        buffers = 0;                                       // (and, when they have been read, the waves' lists)
-        lists = buffers + (size_t)waves * kBuffer * 8;
-        sums = lists + (size_t)beams * pieces * n * 8;
-        tops = sums + (size_t)beams * pieces * 8;
-        tokens = tops + (size_t)beams * pieces * 4;
-        bytes = tokens + (size_t)beams * n * 4;
+        double base = (double)score - log(sum);            // (NaN where the row holds a NaN or an infinity)
+        if (ended) { base = (double)score; top = 0.f; list.key = lane == 0 ? row_key(0.f, a.end_token) : 0; }
+        InAll item{0, ~(unsigned)(k * 64 + lane)};
+        const double t = base + ((double)key_logit(list.key) - (double)top) + 0.0;
+        const u64 u = __builtin_bit_cast(u64, t);
+        if (list.key != 0 && t > -INFINITY) item.key = u >> 63 ? ~u : u | 0x8000000000000000ull;
+        if (lane < a.n_out) tokens[k * a.n_out + lane] = (int)~(unsigned)list.key;
+        if (first) best = item;
+        else join(best, reverse(item));
+        first = false;
+    }
+    // tree: [waves][64] keys and as many words, in LDS
+    __device__ __forceinline__ void finish(int b, int wave, int waves, u64 *tree_keys, unsigned *tree_from)
+    {
+        for (int half = waves / 2; half > 0; half /= 2) {
+            if (wave >= half && wave < 2 * half) { tree_keys[wave * 64 + lane] = best.key; tree_from[wave * 64 + lane] = best.from; }
+            __syncthreads();
+            if (wave < half) join(best, InAll{tree_keys[(wave + half) * 64 + 63 - lane], tree_from[(wave + half) * 64 + 63 - lane]});
+        }
+        if (waves == 1) __syncthreads();                   // (a single wave reads its own tokens)
+        if (wave == 0 && lane < a.n_out) {
+            const long long o = (long long)b * a.n_out + lane;
+            const int from = (int)~best.from, k = from >> 6;
+            const u64 u = best.key >> 63 ? best.key ^ 0x8000000000000000ull : ~best.key;
+            a.scores_out[o] = best.key ? (float)__builtin_bit_cast(double, u) : -INFINITY;
+            a.tokens_out[o] = best.key ? tokens[k * a.n_out + (from & 63)] : -1;
+            a.parents_out[o] = best.key ? k : -1;
+        }
     }
 };
 
-// A work-group an utterance: its waves take its pieces in turn, and join them
+// LDS of a work-group that joins: the waves' buffers or their lists, which take turns, and the tokens
+__host__ __device__ constexpr size_t join_lds(int waves, int beams, int n) { return (size_t)waves * kBuffer * 8 + (size_t)beams * n * 4; }
+
+// A work-group an utterance, its waves take the hypotheses in turn
 template <int TYPE>
 __global__ void __launch_bounds__(kJoinWaves * 64)
 beam_select_kernel(const SelectArgs a)
 {
     extern __shared__ __align__(16) unsigned char lds[];
-    const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const SelectLds l(waves, a.beams, a.pieces, a.n_out);
-    u64 *lists = reinterpret_cast<u64 *>(lds + l.lists);
-    double *sums = reinterpret_cast<double *>(lds + l.sums);
-    float *tops = reinterpret_cast<float *>(lds + l.tops);
-    const int n = a.beams * a.pieces;
-    for (int i = wave; i < n; i += waves)
-        scan_piece<TYPE>(a, (long long)blockIdx.x * n + i, reinterpret_cast<u64 *>(lds + l.buffers) + wave * kBuffer, lists, sums, tops, i);
+    const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), b = blockIdx.x;
+    u64 *buffers = reinterpret_cast<u64 *>(lds);
+    Joined all{a, reinterpret_cast<int *>(buffers + waves * kBuffer), (int)threadIdx.x & 63};
+    for (int k = wave; k < a.beams; k += waves) {
+        auto s = scan_of<typename Logit<TYPE>::T>(a, b, k, buffers + wave * kBuffer);
+        s.begin(0, a.V);                                   // (on their way while the score is read)
+        const float score = a.scores[(long long)b * a.beams + k];
+        const bool ended = a.finished && a.finished[(long long)b * a.beams + k];
+        // nothing of a hypothesis that has ended, or that there is not, is looked at
+        if (!ended && score > -INFINITY) s.run(0, a.V);
+        all.add(k, score, ended, s.list, s.top, s.sum);
+    }
     __syncthreads();
-    u64 *tree = reinterpret_cast<u64 *>(lds + l.buffers);
-    join_rows(a, blockIdx.x, waves, lists, sums, tops, reinterpret_cast<int *>(lds + l.tokens), tree, reinterpret_cast<unsigned *>(tree + waves * 64));
+    all.finish(b, wave, waves, buffers, reinterpret_cast<unsigned *>(buffers + waves * 64));
 }
 
 // Few utterances with long rows: pieces over the whole device, joined by a second launch
@@ -362,19 +337,47 @@ __global__ void __launch_bounds__(256)
 beam_scan_kernel(const SelectArgs a)
 {
     __shared__ u64 buffers[4][kBuffer];
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const long long at = (long long)blockIdx.x * 4 + wave;
-    if (at < (long long)a.B * a.beams * a.pieces) scan_piece<TYPE>(a, at, buffers[wave], a.lists, a.sums, a.tops, at);
+    if (at >= (long long)a.B * a.beams * a.pieces) return;
+    const unsigned hyp = (unsigned)(at / a.pieces), b = hyp / a.beams;
+    const long long from = (at - (long long)hyp * a.pieces) * a.piece_tiles * kTile;
+    const int to = (int)min(from + (long long)a.piece_tiles * kTile, (long long)a.V);
+    auto s = scan_of<typename Logit<TYPE>::T>(a, (int)b, (int)(hyp - b * a.beams), buffers[wave]);
+    s.begin((int)from, to);
+    if ((a.finished && a.finished[hyp]) || !(a.scores[hyp] > -INFINITY)) return;
+    s.run((int)from, to);
+    if (lane < a.n_out) a.lists[at * a.n_out + lane] = s.list.key;
+    if (lane == 0) { a.sums[at] = s.sum; a.tops[at] = s.top; }
 }
 __global__ void __launch_bounds__(kJoinWaves * 64)
 beam_join_kernel(const SelectArgs a)
 {
     extern __shared__ __align__(16) unsigned char lds[];
-    const int waves = blockDim.x >> 6;
-    const long long at = (long long)blockIdx.x * a.beams * a.pieces;
+    const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, b = blockIdx.x, n = a.n_out;
     u64 *tree = reinterpret_cast<u64 *>(lds);
-    unsigned *from = reinterpret_cast<unsigned *>(tree + waves * 64);
-    join_rows(a, blockIdx.x, waves, a.lists + at * a.n_out, a.sums + at, a.tops + at, reinterpret_cast<int *>(from + waves * 64), tree, from);
+    Joined all{a, reinterpret_cast<int *>(tree + waves * kBuffer), lane};
+    for (int k = wave; k < a.beams; k += waves) {
+        const long long hyp = (long long)b * a.beams + k;
+        const float score = a.scores[hyp];
+        const bool ended = a.finished && a.finished[hyp];
+        InRow list{0};
+        float top = kLowest;
+        double sum = 0;
+        if (!ended && score > -INFINITY) {
+            const u64 *mine = a.lists + hyp * a.pieces * n;
+            list.key = lane < n ? mine[lane] : 0;
+            // of the pieces' sums: a lane a piece
+            const float piece_top = lane < a.pieces ? a.tops[hyp * a.pieces + lane] : kLowest;
+            const double piece_sum = lane < a.pieces ? a.sums[hyp * a.pieces + lane] : 0.0;
+            for (int s = 1; s < a.pieces; ++s) join(list, InRow{63 - lane < n ? mine[s * n + 63 - lane] : 0});
+            top = wave_max(piece_top);
+            sum = wave_sum(piece_sum * exp((double)piece_top - (double)top));
+        }
+        all.add(k, score, ended, list, top, sum);
+    }
+    __syncthreads();
+    all.finish(b, wave, waves, tree, reinterpret_cast<unsigned *>(tree + waves * 64));
 }
 
 // A state as the reorder kernel moves it: rows in columns of `width` bytes.  Out of place a work-group takes kItems
@@ -514,10 +517,10 @@ namespace {
 
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
-// How a selection is cut up.  One launch, a work-group an utterance, where that leaves its waves no more than kOneLaunchTiles
-// tiles each and all of it fits LDS: the second launch costs what a wave takes for several tiles.  Else pieces of two tiles or more, towards
-// sixteen waves on every compute unit.
-constexpr int kOneLaunchTiles = 4, kWavesWanted = 4096, kLdsMost = 64 * 1024;
+// How a selection is cut up.  One launch, a work-group an utterance and a wave a row, where that leaves a wave no more than
+// kOneLaunchTiles tiles, or where the rows fill the device: the second launch costs what a wave takes for several tiles.  Else
+// pieces of two tiles or more, towards sixteen waves on every compute unit.
+constexpr int kOneLaunchTiles = 8, kWavesWanted = 4096;
 
 struct SelectPlan {
     bool two = false;
@@ -527,19 +530,13 @@ struct SelectPlan {
     SelectPlan(int64_t B, int beams, int V, int n)
     {
         const int row = (V - 1) / kTile + 1;
-        auto cut = [&](int64_t into) {
-            piece_tiles = (int)((row + into - 1) / into);
-            pieces = (row + piece_tiles - 1) / piece_tiles;
-        };
-        auto waves_for = [&](int jobs) { waves = 1; while (waves < kJoinWaves && waves < jobs) waves *= 2; };
-        cut(std::max(1, kJoinWaves / beams));
-        waves_for(beams * pieces);
-        lds = SelectLds(waves, beams, pieces, n).bytes;
-        if ((beams * pieces + waves - 1) / waves * piece_tiles <= kOneLaunchTiles && lds <= kLdsMost) return;
+        while (waves < kJoinWaves && waves < beams) waves *= 2;
+        lds = join_lds(waves, beams, n);
+        if ((beams + waves - 1) / waves * row <= kOneLaunchTiles || B * beams >= kWavesWanted) return;
         two = true;
-        cut(std::min<int64_t>(std::max<int64_t>(kWavesWanted / (B * beams), 1), std::min(64, (row + 1) / 2)));
-        waves_for(beams);
-        lds = (size_t)waves * 64 * 12 + (size_t)beams * n * 4;
+        const int64_t into = std::min<int64_t>(std::max<int64_t>(kWavesWanted / (B * beams), 1), std::min(64, (row + 1) / 2));
+        piece_tiles = (int)((row + into - 1) / into);
+        pieces = (row + piece_tiles - 1) / piece_tiles;
         bytes = B * beams * pieces * (n * 8 + 12);
     }
 };
