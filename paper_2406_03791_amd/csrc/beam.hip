@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "engine.h"
 
@@ -26,10 +27,10 @@ struct SelectArgs {
     int *tokens_out, *parents_out;
     long long batch_stride, beam_stride;
     int B, beams, V, n_out, end_token;
-    int pieces, piece_tiles;            // a row is cut into so many pieces of so many tiles
-    u64 *lists;                         // [B][beams][pieces][n_out]: the pieces' best,
-    double *sums;                       // [B][beams][pieces]: sums of exponentials
-    float *tops;                        // and the logit that those are relative to
+    // Of two launches: a row is cut into so many pieces for a work-group each, whose waves have so many tiles each
+    int pieces, piece_tiles;
+    u64 *lists;                         // [B][beams][pieces][n_out]: the pieces' best
+    double *sums, *refs;                // [B][beams][pieces][kScanWaves]: sums of exp(x - ref)
 };
 
 // The value of lane ^ M
@@ -90,28 +91,36 @@ template <int M, class Item> __device__ __forceinline__ void exchange(Item &mine
     const bool take = other.above(mine) == better;
     if (take) mine = other;
 }
-// The items of a wave, best first (UP: worst first)
-template <bool UP, class Item> __device__ __forceinline__ void sort_wave(Item &v)
+// Lists are 64 items long, or 16 (WIDTH; lanes 0 .. 15, what the others hold does not matter) where no more are wanted.
+// The items of a wave or of the 16 lanes of a row of it, worst first
+template <int WIDTH, class Item> __device__ __forceinline__ void sort_lanes(Item &v)
 {
     const int lane = threadIdx.x & 63;
-#define RNNT_STEP(K, M) exchange<M>(v, (((lane & M) == 0) == ((lane & K) == 0)) != UP)
+#define RNNT_STEP(K, M) exchange<M>(v, ((lane & M) == 0) != ((lane & K) == 0 || K == WIDTH))
     RNNT_STEP(2, 1);
     RNNT_STEP(4, 2); RNNT_STEP(4, 1);
     RNNT_STEP(8, 4); RNNT_STEP(8, 2); RNNT_STEP(8, 1);
     RNNT_STEP(16, 8); RNNT_STEP(16, 4); RNNT_STEP(16, 2); RNNT_STEP(16, 1);
-    RNNT_STEP(32, 16); RNNT_STEP(32, 8); RNNT_STEP(32, 4); RNNT_STEP(32, 2); RNNT_STEP(32, 1);
-    RNNT_STEP(64, 32); RNNT_STEP(64, 16); RNNT_STEP(64, 8); RNNT_STEP(64, 4); RNNT_STEP(64, 2); RNNT_STEP(64, 1);
+    if constexpr (WIDTH == 64) {
+        RNNT_STEP(32, 16); RNNT_STEP(32, 8); RNNT_STEP(32, 4); RNNT_STEP(32, 2); RNNT_STEP(32, 1);
+        RNNT_STEP(64, 32); RNNT_STEP(64, 16); RNNT_STEP(64, 8); RNNT_STEP(64, 4); RNNT_STEP(64, 2); RNNT_STEP(64, 1);
+    }
 #undef RNNT_STEP
 }
-// The best 64 of a sorted list and of another one that is given worst first, sorted
-template <class Item> __device__ __forceinline__ void join(Item &list, const Item &reversed)
+// The best of a list and of another one that is given worst first, as a list
+template <int WIDTH, class Item> __device__ __forceinline__ void join(Item &list, const Item &reversed)
 {
     const int lane = threadIdx.x & 63;
     if (reversed.above(list)) list = reversed;
-    exchange<32>(list, (lane & 32) == 0); exchange<16>(list, (lane & 16) == 0); exchange<8>(list, (lane & 8) == 0);
-    exchange<4>(list, (lane & 4) == 0); exchange<2>(list, (lane & 2) == 0); exchange<1>(list, (lane & 1) == 0);
+    if constexpr (WIDTH == 64) { exchange<32>(list, (lane & 32) == 0); exchange<16>(list, (lane & 16) == 0); }
+    exchange<8>(list, (lane & 8) == 0); exchange<4>(list, (lane & 4) == 0); exchange<2>(list, (lane & 2) == 0); exchange<1>(list, (lane & 1) == 0);
 }
-template <class Item> __device__ __forceinline__ Item reverse(const Item &v) { return v.template lane<15>().template lane<16>().template lane<32>(); }
+template <int WIDTH, class Item> __device__ __forceinline__ Item reverse(const Item &v)
+{
+    const Item r = v.template lane<15>();
+    if constexpr (WIDTH == 16) return r;
+    else return r.template lane<16>().template lane<32>();
+}
 
 // What lanes of a wave wrote to LDS is there for the others
 __device__ __forceinline__ void wave_sync()
@@ -126,10 +135,11 @@ template <> struct Logit<RNNT_TYPE_BF16> { typedef __bf16 T; };
 template <> struct Logit<RNNT_TYPE_F16> { typedef _Float16 T; };
 
 // Wave-wide maximum and sum
-__device__ __forceinline__ float wave_max(float v)
+template <class F> __device__ __forceinline__ F wave_max(F v)
 {
-    v = fmaxf(v, from_lane<1>(v)); v = fmaxf(v, from_lane<2>(v)); v = fmaxf(v, from_lane<4>(v));
-    v = fmaxf(v, from_lane<8>(v)); v = fmaxf(v, from_lane<16>(v)); return fmaxf(v, from_lane<32>(v));
+    auto larger = [](F a, F b) { if constexpr (sizeof(F) == 4) return fmaxf(a, b); else return fmax(a, b); };
+    v = larger(v, from_lane<1>(v)); v = larger(v, from_lane<2>(v)); v = larger(v, from_lane<4>(v));
+    v = larger(v, from_lane<8>(v)); v = larger(v, from_lane<16>(v)); return larger(v, from_lane<32>(v));
 }
 __device__ __forceinline__ double wave_sum(double v)
 {
@@ -143,8 +153,10 @@ constexpr float kLog2E = 1.44269504f, kLowest = -3.402823466e38f;
 // logits.  A tile is 16 logits a lane (and 64 more where the row ends with them: vocabularies are a power of two and a blank).
 // A tile none of whose logits is above the n-th best so far goes by at the price of one comparison; of the others a lane
 // notes which of its own are, and one a lane at a time they go into a buffer, which is sorted and joined with the list 64 at a time.
+// (LONG: for many tiles; where the buffer has room they go there from the registers, 17 places in the code that are mostly skipped.
+// For a tile or two that costs more in instructions fetched than it saves: 4 rows of 1025 logits take 6.1 us with it and 5.6 without.)
 // Before there is a list, the maxima of n or more groups of lanes bound the n-th best from below.
-template <class T> struct Scan {
+template <class T, int WIDTH, bool LONG> struct Scan {
     static constexpr int PER = 16 / sizeof(T), LOADS = kTile / 64 / PER, ALL = kTile / 64 + 1;
     struct __attribute__((packed, aligned(sizeof(T)))) At { T e[PER]; };
     const T *row;
@@ -153,21 +165,27 @@ template <class T> struct Scan {
     int count = 0;                 // in the buffer
     bool started = false;          // there is a list
     float bar = -INFINITY;         // logits above it are looked at
-    float top = kLowest;           // (never -inf: differences to it are numbers)
-    double sum = 0;
+    // A lane's sum is of 2^(x log2(e) - shift), shift its largest logit times log2(e), rounded.  In the end the sum is the
+    // wave's, of exp(x - ref): what shift was rounded by is in ref.
+    float top = kLowest, shift = kLowest;      // (never -inf: no differences of infinities)
+    double sum = 0, ref = 0;
     InRow list{0};
 
     __device__ __forceinline__ void flush()
     {
         wave_sync();
-        InRow v{lane < count ? buffer[lane] : 0};
-        const u64 rest = lane + 64 < count ? buffer[lane + 64] : 0;
+        const u64 raw = buffer[lane], rest = buffer[lane + 64];
+        InRow v{lane < count ? row_key(__uint_as_float((unsigned)(raw >> 32)), (int)(unsigned)raw) : 0};
         wave_sync();
         buffer[lane] = rest;
+        if (WIDTH == 16 && count <= 16) sort_lanes<16>(v);
+        else {
+            sort_lanes<64>(v);
+            if constexpr (WIDTH == 16) v = v.template lane<16>().template lane<32>();      // the best 16, worst first, to lanes 0 .. 15
+        }
         count = max(count - 64, 0);
-        sort_wave<true>(v);
-        if (started) join(list, v);
-        else list = reverse(v);
+        if (started) join<WIDTH>(list, v);
+        else list = reverse<WIDTH>(v);
         started = true;
         const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(list.key >> 32), n - 1);
         if (hi != 0u) bar = key_logit((u64)hi << 32);
@@ -206,7 +224,9 @@ template <class T> struct Scan {
 #pragma unroll
                 for (int i = 0; i < ALL - 1; ++i) f[i] = (float)next[i / PER].e[i % PER];
                 f[ALL - 1] = kTile + lane < size ? (float)more : -INFINITY;
-                if (rest - size >= kTile) load(base + size, to);
+                // (of many tiles without a branch, which would wait for the loads at its end: with nothing more to load this tile again)
+                if constexpr (LONG) load(rest - size >= kTile ? base + size : base, to);
+                else if (rest - size >= kTile) load(base + size, to);
             } else {
                 T v[ALL - 1];
 #pragma unroll
@@ -218,81 +238,106 @@ template <class T> struct Scan {
             float m = f[0];
 #pragma unroll
             for (int i = 1; i < ALL; ++i) m = fmaxf(m, f[i]);
-            const float high = fmaxf(top, m);
+            top = fmaxf(top, m);
+            const float now = fmaxf(top * kLog2E, kLowest);
             float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < ALL; ++i) part[i % 4] += __builtin_amdgcn_exp2f((f[i] - high) * kLog2E);
-            sum = sum * (double)__builtin_amdgcn_exp2f((top - high) * kLog2E) + (double)((part[0] + part[1]) + (part[2] + part[3]));
-            top = high;
+            for (int i = 0; i < ALL; ++i) part[i % 4] += __builtin_amdgcn_exp2f(__builtin_fmaf(f[i], kLog2E, -now));
+            sum = sum * (double)__builtin_amdgcn_exp2f(shift - now) + (double)((part[0] + part[1]) + (part[2] + part[3]));
+            shift = now;
             if (base == from) first_bar(m);
-            const bool last = size == rest;
-            unsigned mine = 0;                             // a lane's logits above the bar
+            const bool last = size == rest, sort = last || base == from;
+            auto place = [&](int i) { return !full ? i * 64 + lane : i < ALL - 1 ? (i / PER * 64 + lane) * PER + i % PER : kTile + lane; };
+            auto append = [&](bool in, u64 all, float x, int at) {
+                if (in) buffer[count + __builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0u))] = (u64)__float_as_uint(x) << 32 | (unsigned)(base + at);
+                count += __popcll(all);
+            };
+            unsigned mine = 0;                             // a lane's logits above the bar that are to be appended one by one
             if (__ballot(m > bar) != 0ull) {
+                u64 above[ALL];
+                int found = 0;
+                if constexpr (LONG) {
 #pragma unroll
-                for (int i = 0; i < ALL; ++i) mine |= f[i] > bar ? 1u << i : 0u;
+                    for (int i = 0; i < ALL; ++i) { above[i] = __ballot(f[i] > bar); found += __popcll(above[i]); }
+                }
+                if (LONG && count + found <= kBuffer) {
+#pragma unroll
+                    for (int i = 0; i < ALL; ++i) if (above[i] != 0ull) append(f[i] > bar, above[i], f[i], place(i));
+                } else {
+#pragma unroll
+                    for (int i = ALL - 1; i >= 0; --i) mine = mine + mine + (f[i] > bar ? 1u : 0u);
+                }
             }
             for (;;) {
-                const u64 any = __ballot(mine != 0u);
-                if (any != 0ull) {
-                    const int i = __builtin_ctz(mine | 0x80000000u);
-                    const int in_tile = !full ? i * 64 + lane : i < ALL - 1 ? (i / PER * 64 + lane) * PER + i % PER : kTile + lane;
-                    const float x = mine != 0u ? (float)row[base + in_tile] : -INFINITY;
+                const bool more_of_it = __ballot(mine != 0u) != 0ull;
+                if (more_of_it) {
+                    const int at = place(__builtin_ctz(mine | 0x80000000u));
+                    const float x = mine != 0u ? (float)row[base + at] : -INFINITY;
                     // (the bar may have risen to a logit with a higher token)
                     const bool in = mine != 0u && x >= bar;
-                    const u64 all = __ballot(in);
-                    if (in) buffer[count + __builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0u))] = row_key(x, base + in_tile);
-                    count += __popcll(all);
+                    append(in, __ballot(in), x, at);
                     mine &= mine - 1u;
                 }
-                const bool end = any == 0ull;
-                if (count >= 64 || (end && last && count > 0)) flush();
-                if (end) break;
+                if (count >= 64 || (!more_of_it && sort && count > 0)) flush();
+                if (!more_of_it && count < (sort ? 1 : 64)) break;
             }
             base += size;
         }
-        const float all = wave_max(top);
-        sum = wave_sum(sum * (double)__builtin_amdgcn_exp2f((top - all) * kLog2E));
-        top = all;
+        top = wave_max(top);
+        if (!(fabsf(top) < 2.3e38f)) { far(from, to); return; }
+        const float all = wave_max(shift);
+        sum = wave_sum(sum * (double)__builtin_amdgcn_exp2f(shift - all));
+        ref = (double)all / (double)kLog2E;
+    }
+    // A row whose largest logit has a product with log2(e) beyond the largest float (a mask of the type's lowest value, or of -inf, in
+    // all of it; an infinity): the terms are made of differences to the largest logit.
+    __device__ __forceinline__ void far(int from, int to)
+    {
+        sum = 0;
+        for (int j = lane; j < to - from; j += 64) sum += (double)__builtin_amdgcn_exp2f(((float)row[from + j] - top) * kLog2E);
+        sum = wave_sum(sum);
+        ref = (double)top;
     }
 };
 
 // A hypothesis' row or a piece of it
-template <class T> __device__ __forceinline__ Scan<T> scan_of(const SelectArgs &a, int b, int k, u64 *buffer)
+template <class T, int WIDTH, bool LONG> __device__ __forceinline__ Scan<T, WIDTH, LONG> scan_of(const SelectArgs &a, int b, int k, u64 *buffer)
 {
-    Scan<T> s;
+    Scan<T, WIDTH, LONG> s;
     s.row = static_cast<const T *>(a.logits) + b * a.batch_stride + k * a.beam_stride;
     s.buffer = buffer; s.n = a.n_out; s.lane = threadIdx.x & 63;
     return s;
 }
 
 // The waves of a work-group make one list of an utterance's rows: hypothesis by hypothesis with its score, then wave by wave.
-struct Joined {
+template <int WIDTH> struct Joined {
     const SelectArgs &a;
     int *tokens;           // [beams][n_out], in LDS
     int lane;
     InAll best{0, 0};
     bool first = true;
     // the best of hypothesis k; ended: its only candidate is the end token
-    __device__ __forceinline__ void add(int k, float score, bool ended, InRow list, float top, double sum)
+    __device__ __forceinline__ void add(int k, float score, bool ended, InRow list, double ref, double sum)
     {
         double base = (double)score - log(sum);            // (NaN where the row holds a NaN or an infinity)
-        if (ended) { base = (double)score; top = 0.f; list.key = lane == 0 ? row_key(0.f, a.end_token) : 0; }
+        if (ended) { base = (double)score; ref = 0; list.key = lane == 0 ? row_key(0.f, a.end_token) : 0; }
         InAll item{0, ~(unsigned)(k * 64 + lane)};
-        const double t = base + ((double)key_logit(list.key) - (double)top) + 0.0;
+        const double t = base + ((double)key_logit(list.key) - ref) + 0.0;
         const u64 u = __builtin_bit_cast(u64, t);
         if (list.key != 0 && t > -INFINITY) item.key = u >> 63 ? ~u : u | 0x8000000000000000ull;
         if (lane < a.n_out) tokens[k * a.n_out + lane] = (int)~(unsigned)list.key;
         if (first) best = item;
-        else join(best, reverse(item));
+        else join<WIDTH>(best, reverse<WIDTH>(item));
         first = false;
     }
-    // tree: [waves][64] keys and as many words, in LDS
+    // tree: [waves][WIDTH] keys and as many words, in LDS
     __device__ __forceinline__ void finish(int b, int wave, int waves, u64 *tree_keys, unsigned *tree_from)
     {
         for (int half = waves / 2; half > 0; half /= 2) {
-            if (wave >= half && wave < 2 * half) { tree_keys[wave * 64 + lane] = best.key; tree_from[wave * 64 + lane] = best.from; }
+            if (wave >= half && wave < 2 * half && lane < WIDTH) { tree_keys[wave * WIDTH + lane] = best.key; tree_from[wave * WIDTH + lane] = best.from; }
             __syncthreads();
-            if (wave < half) join(best, InAll{tree_keys[(wave + half) * 64 + 63 - lane], tree_from[(wave + half) * 64 + 63 - lane]});
+            const int at = (wave + half) * WIDTH + WIDTH - 1 - lane % WIDTH;
+            if (wave < half) join<WIDTH>(best, InAll{tree_keys[at], tree_from[at]});
         }
         if (waves == 1) __syncthreads();                   // (a single wave reads its own tokens)
         if (wave == 0 && lane < a.n_out) {
@@ -310,71 +355,85 @@ struct Joined {
 __host__ __device__ constexpr size_t join_lds(int waves, int beams, int n) { return (size_t)waves * kBuffer * 8 + (size_t)beams * n * 4; }
 
 // A work-group an utterance, its waves take the hypotheses in turn
-template <int TYPE>
+template <int TYPE, int WIDTH>
 __global__ void __launch_bounds__(kJoinWaves * 64)
 beam_select_kernel(const SelectArgs a)
 {
     extern __shared__ __align__(16) unsigned char lds[];
     const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), b = blockIdx.x;
     u64 *buffers = reinterpret_cast<u64 *>(lds);
-    Joined all{a, reinterpret_cast<int *>(buffers + waves * kBuffer), (int)threadIdx.x & 63};
+    Joined<WIDTH> all{a, reinterpret_cast<int *>(buffers + waves * kBuffer), (int)threadIdx.x & 63};
     for (int k = wave; k < a.beams; k += waves) {
-        auto s = scan_of<typename Logit<TYPE>::T>(a, b, k, buffers + wave * kBuffer);
+        auto s = scan_of<typename Logit<TYPE>::T, WIDTH, false>(a, b, k, buffers + wave * kBuffer);
         s.begin(0, a.V);                                   // (on their way while the score is read)
         const float score = a.scores[(long long)b * a.beams + k];
         const bool ended = a.finished && a.finished[(long long)b * a.beams + k];
         // nothing of a hypothesis that has ended, or that there is not, is looked at
         if (!ended && score > -INFINITY) s.run(0, a.V);
-        all.add(k, score, ended, s.list, s.top, s.sum);
+        all.add(k, score, ended, s.list, s.ref, s.sum);
     }
     __syncthreads();
     all.finish(b, wave, waves, buffers, reinterpret_cast<unsigned *>(buffers + waves * 64));
 }
 
-// Few utterances with long rows: pieces over the whole device, joined by a second launch
-template <int TYPE>
-__global__ void __launch_bounds__(256)
+// Few utterances with long rows: pieces over the whole device, joined by a second launch.  A work-group's waves have four pieces
+// of a row and join them, two by two.
+constexpr int kScanWaves = 4;
+template <int TYPE, int WIDTH>
+__global__ void __launch_bounds__(kScanWaves * 64)
 beam_scan_kernel(const SelectArgs a)
 {
-    __shared__ u64 buffers[4][kBuffer];
+    __shared__ u64 buffers[kScanWaves][kBuffer];
+    __shared__ double sums[kScanWaves], refs[kScanWaves];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const long long at = (long long)blockIdx.x * 4 + wave;
-    if (at >= (long long)a.B * a.beams * a.pieces) return;
-    const unsigned hyp = (unsigned)(at / a.pieces), b = hyp / a.beams;
-    const long long from = (at - (long long)hyp * a.pieces) * a.piece_tiles * kTile;
-    const int to = (int)min(from + (long long)a.piece_tiles * kTile, (long long)a.V);
-    auto s = scan_of<typename Logit<TYPE>::T>(a, (int)b, (int)(hyp - b * a.beams), buffers[wave]);
-    s.begin((int)from, to);
-    if ((a.finished && a.finished[hyp]) || !(a.scores[hyp] > -INFINITY)) return;
-    s.run((int)from, to);
-    if (lane < a.n_out) a.lists[at * a.n_out + lane] = s.list.key;
-    if (lane == 0) { a.sums[at] = s.sum; a.tops[at] = s.top; }
+    const unsigned hyp = blockIdx.x / a.pieces, b = hyp / a.beams;
+    const long long piece = (long long)(blockIdx.x - hyp * a.pieces) * kScanWaves + wave;
+    const int from = (int)min(piece * a.piece_tiles * kTile, (long long)a.V), to = (int)min((piece + 1) * a.piece_tiles * kTile, (long long)a.V);
+    auto s = scan_of<typename Logit<TYPE>::T, WIDTH, true>(a, (int)b, (int)(hyp - b * a.beams), buffers[wave]);
+    s.begin(from, to);
+    if ((a.finished && a.finished[hyp]) || !(a.scores[hyp] > -INFINITY)) return;       // (the whole work-group)
+    s.run(from, to);
+    if (lane == 0) { sums[wave] = s.sum; refs[wave] = s.ref; }
+    for (int half = kScanWaves / 2; half > 0; half /= 2) {
+        if (wave >= half && wave < 2 * half && lane < WIDTH) buffers[wave][lane] = s.list.key;
+        __syncthreads();
+        if (wave < half) join<WIDTH>(s.list, InRow{buffers[wave + half][WIDTH - 1 - lane % WIDTH]});
+    }
+    if (wave != 0) return;
+    if (lane < a.n_out) a.lists[(long long)blockIdx.x * a.n_out + lane] = s.list.key;
+    if (lane < kScanWaves) { a.sums[(long long)blockIdx.x * kScanWaves + lane] = sums[lane]; a.refs[(long long)blockIdx.x * kScanWaves + lane] = refs[lane]; }
 }
+template <int WIDTH>
 __global__ void __launch_bounds__(kJoinWaves * 64)
 beam_join_kernel(const SelectArgs a)
 {
     extern __shared__ __align__(16) unsigned char lds[];
     const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, b = blockIdx.x, n = a.n_out;
     u64 *tree = reinterpret_cast<u64 *>(lds);
-    Joined all{a, reinterpret_cast<int *>(tree + waves * kBuffer), lane};
+    Joined<WIDTH> all{a, reinterpret_cast<int *>(tree + waves * kBuffer), lane};
     for (int k = wave; k < a.beams; k += waves) {
         const long long hyp = (long long)b * a.beams + k;
+        // (asked for together, whether they are there or not: the tables are)
+        const u64 *mine = a.lists + hyp * a.pieces * n;
+        const u64 first = mine[min(lane, n - 1)];
+        const bool mine_too = lane < a.pieces * kScanWaves;
+        const long long sum_at = hyp * a.pieces * kScanWaves + (mine_too ? lane : 0);
+        const double piece_ref = a.refs[sum_at], piece_sum = a.sums[sum_at];
         const float score = a.scores[hyp];
         const bool ended = a.finished && a.finished[hyp];
         InRow list{0};
-        float top = kLowest;
-        double sum = 0;
+        double ref = 0, sum = 0;
         if (!ended && score > -INFINITY) {
-            const u64 *mine = a.lists + hyp * a.pieces * n;
-            list.key = lane < n ? mine[lane] : 0;
-            // of the pieces' sums: a lane a piece
-            const float piece_top = lane < a.pieces ? a.tops[hyp * a.pieces + lane] : kLowest;
-            const double piece_sum = lane < a.pieces ? a.sums[hyp * a.pieces + lane] : 0.0;
-            for (int s = 1; s < a.pieces; ++s) join(list, InRow{63 - lane < n ? mine[s * n + 63 - lane] : 0});
-            top = wave_max(piece_top);
-            sum = wave_sum(piece_sum * exp((double)piece_top - (double)top));
+            list.key = lane < n ? first : 0;
+            for (int s = 1; s < a.pieces; ++s) {
+                const int at = WIDTH - 1 - lane % WIDTH;
+                join<WIDTH>(list, InRow{at < n ? mine[s * n + at] : 0});
+            }
+            // (a wave without logits has a sum of 0)
+            ref = wave_max(mine_too && piece_sum != 0.0 ? piece_ref : -(double)INFINITY);
+            sum = wave_sum(mine_too && piece_sum != 0.0 ? piece_sum * exp(piece_ref - ref) : 0.0);
         }
-        all.add(k, score, ended, list, top, sum);
+        all.add(k, score, ended, list, ref, sum);
     }
     __syncthreads();
     all.finish(b, wave, waves, tree, reinterpret_cast<unsigned *>(tree + waves * 64));
@@ -534,10 +593,10 @@ struct SelectPlan {
         lds = join_lds(waves, beams, n);
         if ((beams + waves - 1) / waves * row <= kOneLaunchTiles || B * beams >= kWavesWanted) return;
         two = true;
-        const int64_t into = std::min<int64_t>(std::max<int64_t>(kWavesWanted / (B * beams), 1), std::min(64, (row + 1) / 2));
-        piece_tiles = (int)((row + into - 1) / into);
-        pieces = (row + piece_tiles - 1) / piece_tiles;
-        bytes = B * beams * pieces * (n * 8 + 12);
+        const int64_t into = std::min<int64_t>(std::max<int64_t>(kWavesWanted / (B * beams * kScanWaves), 1), std::min(64 / kScanWaves, (row + 2 * kScanWaves - 1) / (2 * kScanWaves)));
+        piece_tiles = (int)((row + into * kScanWaves - 1) / (into * kScanWaves));
+        pieces = (row + piece_tiles * kScanWaves - 1) / (piece_tiles * kScanWaves);
+        bytes = B * beams * pieces * (n * 8 + kScanWaves * 16);
     }
 };
 
@@ -575,23 +634,26 @@ int rnnt_beam_select(const void *logits, int32_t type, int64_t batch_stride, int
     const hipStream_t on = static_cast<hipStream_t>(stream);
     if (!p.two) {
         auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(B), dim3(p.waves * 64), (unsigned)p.lds, on, args); };
-        if (type == RNNT_TYPE_F32) run(beam_select_kernel<RNNT_TYPE_F32>);
-        else if (type == RNNT_TYPE_BF16) run(beam_select_kernel<RNNT_TYPE_BF16>);
-        else run(beam_select_kernel<RNNT_TYPE_F16>);
+        auto with = [&](auto t) { if (n_out <= 16) run(beam_select_kernel<t(), 16>); else run(beam_select_kernel<t(), 64>); };
+        if (type == RNNT_TYPE_F32) with(std::integral_constant<int, RNNT_TYPE_F32>());
+        else if (type == RNNT_TYPE_BF16) with(std::integral_constant<int, RNNT_TYPE_BF16>());
+        else with(std::integral_constant<int, RNNT_TYPE_F16>());
         BEAM_TRY(hipGetLastError());
         return RNNT_OK;
     }
     const int64_t n = (int64_t)B * beams * p.pieces;
+    if (n > 0x7fffffff) return RNNT_ERR_UNSUPPORTED;
     args.lists = static_cast<u64 *>(workspace);
     args.sums = reinterpret_cast<double *>(args.lists + n * n_out);
-    args.tops = reinterpret_cast<float *>(args.sums + n);
-    if ((n + 3) / 4 > 0x7fffffff) return RNNT_ERR_UNSUPPORTED;
-    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, on, args); };
-    if (type == RNNT_TYPE_F32) run(beam_scan_kernel<RNNT_TYPE_F32>);
-    else if (type == RNNT_TYPE_BF16) run(beam_scan_kernel<RNNT_TYPE_BF16>);
-    else run(beam_scan_kernel<RNNT_TYPE_F16>);
+    args.refs = args.sums + n * kScanWaves;
+    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(kScanWaves * 64), 0, on, args); };
+    auto with = [&](auto t) { if (n_out <= 16) run(beam_scan_kernel<t(), 16>); else run(beam_scan_kernel<t(), 64>); };
+    if (type == RNNT_TYPE_F32) with(std::integral_constant<int, RNNT_TYPE_F32>());
+    else if (type == RNNT_TYPE_BF16) with(std::integral_constant<int, RNNT_TYPE_BF16>());
+    else with(std::integral_constant<int, RNNT_TYPE_F16>());
     BEAM_TRY(hipGetLastError());
-    hipLaunchKernelGGL(beam_join_kernel, dim3(B), dim3(p.waves * 64), (unsigned)p.lds, on, args);
+    auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(B), dim3(p.waves * 64), (unsigned)p.lds, on, args); };
+    if (n_out <= 16) join(beam_join_kernel<16>); else join(beam_join_kernel<64>);
     BEAM_TRY(hipGetLastError());
     return RNNT_OK;
 }
