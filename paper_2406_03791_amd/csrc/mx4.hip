@@ -326,16 +326,16 @@ mx4_tile_kernel(const ProductArgs g, int m_blocks, int n_blocks)
         const unsigned m = (unsigned)__builtin_amdgcn_readfirstlane((int)(lds0 + to));
         asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" :: "v"(off), "s"(m), "s"(from) : "memory");
     };
-    // pieces of step s (beyond the end those of the last one again, so that every step has as many) to stage `at`
-    auto ask = [&](int s, int at, bool with_scales) {
+    // pieces of step s (beyond the end those of the last one again, so that every step has as many) to stage `at`: those of scales first
+    auto ask_one = [&](int s, int at, int i) {
         const long long k = min(s, steps - 1);
-        if (with_scales) {
+        if (i < 0) to_lds(uniform(scale[i + SCALE_LOADS] + k / 4 * kScaleBytes), scale_off[i + SCALE_LOADS],
+                          (unsigned)(S::STAGES * S::CODES + (s / 4 & 1) * S::SCALES + (wave * SCALE_LOADS + i + SCALE_LOADS) * 1024));
+        else to_lds(uniform(code[i] + k * kTileBytes), (unsigned)lane * 16u, (unsigned)(at * S::CODES + (wave * LOADS + i) * kTileBytes));
+    };
+    auto ask = [&](int s, int at, bool with_scales) {
 #pragma unroll
-            for (int i = 0; i < SCALE_LOADS; ++i)
-                to_lds(uniform(scale[i] + k / 4 * kScaleBytes), scale_off[i], (unsigned)(S::STAGES * S::CODES + (s / 4 & 1) * S::SCALES + (wave * SCALE_LOADS + i) * 1024));
-        }
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) to_lds(uniform(code[i] + k * kTileBytes), (unsigned)lane * 16u, (unsigned)(at * S::CODES + (wave * LOADS + i) * kTileBytes));
+        for (int i = -SCALE_LOADS; i < LOADS; ++i) if (i >= 0 || with_scales) ask_one(s, at, i);
     };
     const int wm = wave & 1, wn = wave >> 1;
     // a lane's operand of 32 rows and half h of a tile: rows lane % 32, block 2 h + lane / 32
@@ -345,20 +345,23 @@ mx4_tile_kernel(const ProductArgs g, int m_blocks, int n_blocks)
     auto read_scale = [&](int group, int tile, int h) { return *reinterpret_cast<const int *>(mine_s + (group & 1) * S::SCALES + tile * kScaleBytes + h * 128); };
     struct Half { v4u a[TM], w[TN]; };
     struct Scales { int a[2][TM], w[2][TN]; };
+    auto read_one = [&](Half &o, int stage, int h, int i) {
+        if (i < TM) o.a[i] = read(stage, wm * TM * 2 + i * 2, h);
+        else o.w[i - TM] = read(stage, S::BM / 16 + wn * TN * 2 + (i - TM) * 2, h);
+    };
     auto read_half = [&](Half &o, int stage, int h) {
 #pragma unroll
-        for (int i = 0; i < TM; ++i) o.a[i] = read(stage, wm * TM * 2 + i * 2, h);
-#pragma unroll
-        for (int i = 0; i < TN; ++i) o.w[i] = read(stage, S::BM / 16 + wn * TN * 2 + i * 2, h);
+        for (int i = 0; i < TM + TN; ++i) read_one(o, stage, h, i);
+    };
+    auto read_scale_one = [&](Scales &o, int group, int h, int i) {
+        if (i < TM) o.a[h][i] = read_scale(group, wm * TM * 2 + i * 2, h);
+        else o.w[h][i - TM] = read_scale(group, S::BM / 16 + wn * TN * 2 + (i - TM) * 2, h);
     };
     auto read_scales = [&](Scales &o, int group) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < TM; ++i) o.a[h][i] = read_scale(group, wm * TM * 2 + i * 2, h);
-#pragma unroll
-            for (int i = 0; i < TN; ++i) o.w[h][i] = read_scale(group, S::BM / 16 + wn * TN * 2 + i * 2, h);
-        }
+            for (int i = 0; i < TM + TN; ++i) read_scale_one(o, group, h, i);
     };
     v16f sum[TN][TM];
 #pragma unroll
@@ -376,24 +379,37 @@ mx4_tile_kernel(const ProductArgs g, int m_blocks, int n_blocks)
         asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(2 * LOADS) : "memory");
         read_scales(now, 0);
         read_half(half[0], 0, 0);
+        // A matrix instruction takes 32 cycles, others go beside it: one thing is asked for or read behind each.
+        constexpr int ALL = TM * TN, READS = TM + TN, EACH = (2 * READS + ALL - 1) / ALL;
         auto step = [&](int t, auto number) {
             constexpr int I = decltype(number)::value;     // t % 4
-            read_half(half[1], I, 1);
 #pragma unroll
-            for (int i = 0; i < TN; ++i)
+            for (int e = 0; e < ALL; ++e) {
+                const int i = e / TM, j = e % TM;
+                sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(half[0].w[i]), operand(half[0].a[j]), sum[i][j], 4, 4, I, now.w[0][i], I, now.a[0][j]);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int j = 0; j < TM; ++j)
-                    sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(half[0].w[i]), operand(half[0].a[j]), sum[i][j], 4, 4, I, now.w[0][i], I, now.a[0][j]);
+                for (int r = e * EACH; r < (e + 1) * EACH; ++r) if (r < READS) read_one(half[1], I, 1, r);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             // what step t + 1 needs is there; of step t + 2 it may still be on its way
             asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(LOADS + (I == 2 ? SCALE_LOADS : 0)) : "memory");
-            ask(t + 3, (I + 3) % 4, I == 1);
-            if constexpr (I == 3) read_scales(next, t / 4 + 1);
-            read_half(half[0], (I + 1) % 4, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            constexpr int FIRST = I == 1 ? -SCALE_LOADS : 0, ASKS = LOADS - FIRST, PER_ASK = (2 * ASKS + ALL - 1) / ALL;
 #pragma unroll
-            for (int i = 0; i < TN; ++i)
+            for (int e = 0; e < ALL; ++e) {
+                const int i = e / TM, j = e % TM;
+                sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(half[1].w[i]), operand(half[1].a[j]), sum[i][j], 4, 4, I, now.w[1][i], I, now.a[1][j]);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int j = 0; j < TM; ++j)
-                    sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(half[1].w[i]), operand(half[1].a[j]), sum[i][j], 4, 4, I, now.w[1][i], I, now.a[1][j]);
+                for (int r = e * EACH; r < (e + 1) * EACH; ++r) {
+                    if (r < READS) read_one(half[0], (I + 1) % 4, 0, r);
+                    if (I == 3 && r < READS) { read_scale_one(next, t / 4 + 1, 0, r); read_scale_one(next, t / 4 + 1, 1, r); }
+                }
+#pragma unroll
+                for (int r = e * PER_ASK; r < (e + 1) * PER_ASK; ++r) if (r < ASKS) ask_one(t + 3, (I + 3) % 4, FIRST + r);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             if constexpr (I == 3) now = next;
         };
         for (int t = 0; t < steps; t += 4) {
@@ -402,24 +418,38 @@ mx4_tile_kernel(const ProductArgs g, int m_blocks, int n_blocks)
             if (t + 2 < steps) step(t + 2, std::integral_constant<int, 2>());
             if (t + 3 < steps) step(t + 3, std::integral_constant<int, 3>());
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing is on its way to LDS that is given up)
+        // (nothing is on its way to LDS or read there that the results would meet)
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
     }
-    // Register v of lane l holds row 8 (v / 4) + 4 (l / 32) + v % 4 of w's 32, row l % 32 of a's.
+    // Results leave by way of a wave's own part of LDS, 32 rows of y at a time, so that whole rows of the wave's columns are stored:
+    // register v of lane l holds row 8 (v / 4) + 4 (l / 32) + v % 4 of w's 32, row l % 32 of a's.  (Straight from the registers, sixteen
+    // bytes a row and store, this took 80 of 290 us of a product of 8192^3, for its stores and for fetching its code.)
+    constexpr int COLS = TN * 32, PITCH = COLS + 4, LANES = COLS / 4, ROWS = 64 / LANES;
+    static_assert(4 * 32 * PITCH * 4 <= S::LDS, "the waves' parts fit");
+    float *part = reinterpret_cast<float *>(lds) + wave * (32 * PITCH);
+    const int n = nb * S::BN + wn * COLS + lane % LANES * 4, left = g.N - n;
+    float bias[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bias[e] = g.bias && e < left ? g.bias[n + e] : 0.f;
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
-        const long long m = (long long)mb * S::BM + wm * TM * 32 + j * 32 + (lane & 31);
-        if (m >= g.M) continue;
+        asm volatile("" ::: "memory");
 #pragma unroll
         for (int i = 0; i < TN; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const long long n = (long long)nb * S::BN + wn * TN * 32 + i * 32 + q * 8 + (lane >> 5) * 4;
-                if (n >= g.N) continue;
-                float o[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = sum[i][j][q * 4 + e] + (g.bias && n + e < g.N ? g.bias[n + e] : 0.f);
-                store_four(g.y, g.y_type, m * g.y_stride + n, o, g.N - n);
-            }
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<v4f *>(part + (lane & 31) * PITCH + i * 32 + q * 8 + (lane >> 5) * 4) =
+                    v4f{sum[i][j][q * 4], sum[i][j][q * 4 + 1], sum[i][j][q * 4 + 2], sum[i][j][q * 4 + 3]};
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        const int m0 = mb * S::BM + wm * TM * 32 + j * 32, rows = min(32, g.M - m0);
+        if (left <= 0) continue;
+#pragma unroll 4
+        for (int r = lane / LANES; r < rows; r += ROWS) {
+            const v4f v = *reinterpret_cast<const v4f *>(part + r * PITCH + lane % LANES * 4);
+            const float o[4] = {v.x + bias[0], v.y + bias[1], v.z + bias[2], v.w + bias[3]};
+            store_four(g.y, g.y_type, (long long)(m0 + r) * g.y_stride + n, o, left);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 }
 
