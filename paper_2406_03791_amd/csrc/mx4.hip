@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "engine.h"
@@ -265,6 +266,13 @@ mx4_product_kernel(const ProductArgs g)
     store_four(g.y, g.y_type, ((long long)mt * kTileRows + m) * g.y_stride + n, o, g.N - n);
 }
 
+// What lanes of a wave wrote to LDS is there for the others
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 __device__ __forceinline__ const unsigned char *uniform(const unsigned char *p)
 {
     const unsigned long long u = reinterpret_cast<unsigned long long>(p);
@@ -272,185 +280,262 @@ __device__ __forceinline__ const unsigned char *uniform(const unsigned char *p)
     return reinterpret_cast<const unsigned char *>((unsigned long long)hi << 32 | lo);
 }
 
-// Many rows: bound by the matrix instructions, 32 cycles for 32 x 32 x 64.  A work-group is 2 x 2 waves of TN x TM tiles
-// of 32 x 32 outputs (rows of w by rows of a).  Tiles of codes lie in memory as the lanes take them: they go to LDS in pieces of
-// 1 KB, four tiles of K in turn (STAGES), and from there to registers without bank conflicts.
+// Many rows: bound by the matrix instructions, 32 cycles for 32 x 32 x 64 (and, in long products, by what the card may draw: those
+// instructions alone, on random codes, reach 6.6 PFLOP/s here, on zeros 9.5).  A block of y, BM x BN outputs, is that of 2 x 2 waves
+// with TM x TN tiles of 32 x 32 each.  Tiles of codes lie in memory as the lanes take them: they go to LDS in pieces of 1 KB, STAGES
+// tiles of K in turn, and from there to registers without bank conflicts.
 //
+// A work-group has a block after the other, and asks for pieces of the next one while it is still at this one: the
+// pipeline does not run dry between blocks, and results are on their way to memory while the next block is multiplied.
 // In a step (a tile of K, two instructions deep) the operands of the second half are read while the first half is
-// multiplied; then the wave waits for the next step's pieces, of which a step's time has passed since they were asked for, meets the others,
-// asks for the pieces three steps ahead (their place was last read a step ago), and reads the next step's first half while the second is
-// multiplied.  Scales: four steps' in a word, in LDS twice, asked for with the first step's codes.
-template <int TM, int TN>
+// multiplied; then the wave waits for the next step's pieces, meets the others, asks for the pieces STAGES - 1 steps
+// ahead (their place was last read a step ago), and reads the next step's first half while the second is multiplied.
+// Between matrix instructions there is room for others: one thing is asked for or read behind each.  Scales: four steps' in a word,
+// asked for with the first step's codes.
+// CHAIN: a work-group has several blocks, and the results a place of their own in LDS; else it has one, and they take that of the codes.
+template <int TM_, int TN_, int STAGES_, bool CHAIN_>
 struct TileShape {
-    static constexpr int BM = TM * 64, BN = TN * 64, TILES = (BM + BN) / kTileRows, STAGES = 4;
-    static constexpr int CODES = TILES * kTileBytes, SCALES = TILES * kScaleBytes, LDS = STAGES * CODES + 2 * SCALES;
+    static constexpr int TM = TM_, TN = TN_, STAGES = STAGES_;
+    static constexpr bool CHAIN = CHAIN_;
+    static constexpr int BM = TM * 64, BN = TN * 64, TILES = (BM + BN) / kTileRows;
+    static constexpr int CODES = TILES * kTileBytes, SCALES = TILES * kScaleBytes, OUT = CHAIN ? 4 * 4096 : 0;
+    static constexpr int LDS = STAGES * CODES + 2 * SCALES + OUT, GROUPS = 160 * 1024 / LDS;      // work-groups of a compute unit
 };
 
-template <int TM, int TN>
-__global__ void __launch_bounds__(256)
+template <class S, int Y>
+__global__ void __launch_bounds__(256, S::GROUPS)
 mx4_tile_kernel(const ProductArgs g, int m_blocks, int n_blocks)
 {
-    typedef TileShape<TM, TN> S;
-    constexpr int LOADS = S::TILES / 4, SCALE_LOADS = S::TILES / 16;       // of a wave: a tile of codes each, four tiles' scales each
-    static_assert(S::TILES % 16 == 0, "whole loads for four waves");
+    typedef typename Element<Y>::T YT;
+    constexpr int TM = S::TM, TN = S::TN, STAGES = S::STAGES;
+    constexpr int LOADS = S::TILES / 4, SCALE_LOADS = S::TILES / 16;       // of a wave: a tile of codes a load, four tiles' scales a load
+    static_assert(S::TILES % 16 == 0 && S::BM % 64 == 0, "whole loads, of one operand each");
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int steps = (int)tiles(g.K, kTileCols), groups = (int)tiles(g.K, kScaleCols);
-    // Blocks of an XCD follow each other, in bands of eight blocks of rows of a, so that its L2 serves each operand to several.
-    int mb, nb;
-    {
-        const int n = m_blocks * n_blocks, xcd = blockIdx.x & 7, at = xcd * (n / 8) + min(xcd, n % 8) + (blockIdx.x >> 3);
-        const int band = at / (8 * n_blocks), in = at - band * 8 * n_blocks, high = min(8, m_blocks - band * 8);
-        nb = in / high;
-        mb = band * 8 + in - nb * high;
-    }
     const int m_last = (int)tiles(g.M, kTileRows) - 1, n_last = (int)tiles(g.N, kTileRows) - 1;
-    // row of tiles number i of the block: first those of a, then those of w; what is beyond the end repeats the last one and is not stored
-    auto tile_row = [&](int i) { return i < S::BM / 16 ? min(mb * (S::BM / 16) + i, m_last) : min(nb * (S::BN / 16) + i - S::BM / 16, n_last); };
-    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds;
+    // An XCD has blocks that follow each other, in bands of eight blocks of rows of a, so that its L2 serves each operand to several
+    // work-groups; those of it take them in turn.
+    const int n_all = m_blocks * n_blocks, xcd = blockIdx.x & 7, here = n_all / 8 + (xcd < n_all % 8), peers = ((int)gridDim.x - xcd + 7) / 8;
+    struct Block { int mb, nb; };
+    auto block = [&](int i) {
+        const int at = xcd * (n_all / 8) + min(xcd, n_all % 8) + i;
+        const int band = at / (8 * n_blocks), in = at - band * 8 * n_blocks, high = min(8, m_blocks - band * 8);
+        return Block{band * 8 + in % high, in / high};
+    };
+    // What is asked for: pieces of step ask_step of block ask_block, from `code` and `scale` on
+    int ask_block = blockIdx.x >> 3, ask_step = 0, ask_group = 0;
+    if (ask_block >= here) return;
     const unsigned char *code[LOADS], *scale[SCALE_LOADS];
     unsigned scale_off[SCALE_LOADS];
+    auto aim = [&]() {
+        const Block k = block(ask_block);
+        // row of tiles number i of the block: first those of a, then those of w; what is beyond the end repeats the last one and is not stored
+        auto tile_row = [&](int i) { return i < S::BM / 16 ? min(k.mb * (S::BM / 16) + i, m_last) : min(k.nb * (S::BN / 16) + i - S::BM / 16, n_last); };
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-        const int t = wave * LOADS + i;
-        code[i] = uniform((t < S::BM / 16 ? static_cast<const unsigned char *>(g.a) : g.w) + (long long)tile_row(t) * steps * kTileBytes);
-    }
+        for (int i = 0; i < LOADS; ++i) {
+            const int t = wave * LOADS + i;
+            code[i] = uniform((t < S::BM / 16 ? static_cast<const unsigned char *>(g.a) : g.w) + (long long)tile_row(t) * steps * kTileBytes);
+        }
 #pragma unroll
-    for (int i = 0; i < SCALE_LOADS; ++i) {
-        // (four rows of tiles of one operand: their first one's address, and a lane's distance from it)
-        const int t = (wave * SCALE_LOADS + i) * 4, first = tile_row(t);
-        scale[i] = uniform((t < S::BM / 16 ? g.a_scales : g.w_scales) + (long long)first * groups * kScaleBytes);
-        scale_off[i] = (unsigned)(tile_row(t + (lane >> 4)) - first) * (unsigned)groups * kScaleBytes + (lane & 15) * 16;
-    }
+        for (int i = 0; i < SCALE_LOADS; ++i) {
+            // (four rows of tiles of one operand: their first one's address, and a lane's distance from it)
+            const int t = (wave * SCALE_LOADS + i) * 4, first = tile_row(t);
+            scale[i] = uniform((t < S::BM / 16 ? g.a_scales : g.w_scales) + (long long)first * groups * kScaleBytes);
+            scale_off[i] = (unsigned)(tile_row(t + (lane >> 4)) - first) * (unsigned)groups * kScaleBytes + (lane & 15) * 16;
+        }
+    };
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds;
     auto to_lds = [&](const unsigned char *from, unsigned off, unsigned to) {
         const unsigned m = (unsigned)__builtin_amdgcn_readfirstlane((int)(lds0 + to));
         asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" :: "v"(off), "s"(m), "s"(from) : "memory");
     };
-    // pieces of step s (beyond the end those of the last one again, so that every step has as many) to stage `at`: those of scales first
-    auto ask_one = [&](int s, int at, int i) {
-        const long long k = min(s, steps - 1);
-        if (i < 0) to_lds(uniform(scale[i + SCALE_LOADS] + k / 4 * kScaleBytes), scale_off[i + SCALE_LOADS],
-                          (unsigned)(S::STAGES * S::CODES + (s / 4 & 1) * S::SCALES + (wave * SCALE_LOADS + i + SCALE_LOADS) * 1024));
-        else to_lds(uniform(code[i] + k * kTileBytes), (unsigned)lane * 16u, (unsigned)(at * S::CODES + (wave * LOADS + i) * kTileBytes));
-    };
-    auto ask = [&](int s, int at, bool with_scales) {
+    auto ask_scales = [&]() {
+        if (ask_step % 4 != 0) return;
 #pragma unroll
-        for (int i = -SCALE_LOADS; i < LOADS; ++i) if (i >= 0 || with_scales) ask_one(s, at, i);
+        for (int i = 0; i < SCALE_LOADS; ++i)
+            to_lds(uniform(scale[i] + (long long)(ask_step / 4) * kScaleBytes), scale_off[i],
+                   (unsigned)(STAGES * S::CODES + (ask_group & 1) * S::SCALES + (wave * SCALE_LOADS + i) * 1024));
+        ++ask_group;
+    };
+    auto ask_code = [&](int stage, int i) {
+        to_lds(uniform(code[i] + (long long)ask_step * kTileBytes), (unsigned)lane * 16u, (unsigned)(stage * S::CODES + (wave * LOADS + i) * kTileBytes));
+    };
+    // the step behind; behind the last block's last one its first again, which nobody reads
+    auto advance = [&]() {
+        if (++ask_step < steps) return;
+        ask_step = 0;
+        if constexpr (S::CHAIN) {
+            if (ask_block + peers < here) ask_block += peers;
+            aim();
+        }
     };
     const int wm = wave & 1, wn = wave >> 1;
     // a lane's operand of 32 rows and half h of a tile: rows lane % 32, block 2 h + lane / 32
     const unsigned char *mine = lds + (lane >> 4 & 1) * kTileBytes + (lane >> 5) * 256 + (lane & 15) * 16;
-    auto read = [&](int stage, int tile, int h) { return *reinterpret_cast<const v4u *>(mine + stage * S::CODES + tile * kTileBytes + h * 512); };
-    const unsigned char *mine_s = lds + S::STAGES * S::CODES + (lane >> 4 & 1) * kScaleBytes + (lane >> 5) * 64 + (lane & 15) * 4;
-    auto read_scale = [&](int group, int tile, int h) { return *reinterpret_cast<const int *>(mine_s + (group & 1) * S::SCALES + tile * kScaleBytes + h * 128); };
+    const unsigned char *mine_s = lds + STAGES * S::CODES + (lane >> 4 & 1) * kScaleBytes + (lane >> 5) * 64 + (lane & 15) * 4;
     struct Half { v4u a[TM], w[TN]; };
-    struct Scales { int a[2][TM], w[2][TN]; };
+    struct Scales { int a[2][TM], w[2][TN]; };             // of four steps, the step's own in the lowest byte
+    auto tile_of = [&](int i) { return i < TM ? wm * TM * 2 + i * 2 : S::BM / 16 + wn * TN * 2 + (i - TM) * 2; };
     auto read_one = [&](Half &o, int stage, int h, int i) {
-        if (i < TM) o.a[i] = read(stage, wm * TM * 2 + i * 2, h);
-        else o.w[i - TM] = read(stage, S::BM / 16 + wn * TN * 2 + (i - TM) * 2, h);
-    };
-    auto read_half = [&](Half &o, int stage, int h) {
-#pragma unroll
-        for (int i = 0; i < TM + TN; ++i) read_one(o, stage, h, i);
-    };
-    auto read_scale_one = [&](Scales &o, int group, int h, int i) {
-        if (i < TM) o.a[h][i] = read_scale(group, wm * TM * 2 + i * 2, h);
-        else o.w[h][i - TM] = read_scale(group, S::BM / 16 + wn * TN * 2 + (i - TM) * 2, h);
+        const v4u v = *reinterpret_cast<const v4u *>(mine + stage * S::CODES + tile_of(i) * kTileBytes + h * 512);
+        if (i < TM) o.a[i] = v; else o.w[i - TM] = v;
     };
     auto read_scales = [&](Scales &o, int group) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < TM + TN; ++i) read_scale_one(o, group, h, i);
+            for (int i = 0; i < TM + TN; ++i) {
+                const int v = *reinterpret_cast<const int *>(mine_s + (group & 1) * S::SCALES + tile_of(i) * kScaleBytes + h * 128);
+                if (i < TM) o.a[h][i] = v; else o.w[h][i - TM] = v;
+            }
     };
-    v16f sum[TN][TM];
+    auto shift = [&](Scales &o) {
 #pragma unroll
-    for (int i = 0; i < TN; ++i)
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int j = 0; j < TM; ++j)
+            for (int i = 0; i < TM; ++i) o.a[h][i] = (int)((unsigned)o.a[h][i] >> 8);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sum[i][j][e] = 0.f;
-    if (steps > 0) {
-        Half half[2];
-        Scales now, next;
-        ask(0, 0, true);
-        ask(1, 1, false);
-        ask(2, 2, false);
-        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(2 * LOADS) : "memory");
-        read_scales(now, 0);
-        read_half(half[0], 0, 0);
-        // A matrix instruction takes 32 cycles, others go beside it: one thing is asked for or read behind each.
-        constexpr int ALL = TM * TN, READS = TM + TN, EACH = (2 * READS + ALL - 1) / ALL;
-        auto step = [&](int t, auto number) {
-            constexpr int I = decltype(number)::value;     // t % 4
-#pragma unroll
-            for (int e = 0; e < ALL; ++e) {
-                const int i = e / TM, j = e % TM;
-                sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(half[0].w[i]), operand(half[0].a[j]), sum[i][j], 4, 4, I, now.w[0][i], I, now.a[0][j]);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int r = e * EACH; r < (e + 1) * EACH; ++r) if (r < READS) read_one(half[1], I, 1, r);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            // what step t + 1 needs is there; of step t + 2 it may still be on its way
-            asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(LOADS + (I == 2 ? SCALE_LOADS : 0)) : "memory");
-            __builtin_amdgcn_sched_barrier(0);
-            constexpr int FIRST = I == 1 ? -SCALE_LOADS : 0, ASKS = LOADS - FIRST, PER_ASK = (2 * ASKS + ALL - 1) / ALL;
-#pragma unroll
-            for (int e = 0; e < ALL; ++e) {
-                const int i = e / TM, j = e % TM;
-                sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(half[1].w[i]), operand(half[1].a[j]), sum[i][j], 4, 4, I, now.w[1][i], I, now.a[1][j]);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int r = e * EACH; r < (e + 1) * EACH; ++r) {
-                    if (r < READS) read_one(half[0], (I + 1) % 4, 0, r);
-                    if (I == 3 && r < READS) { read_scale_one(next, t / 4 + 1, 0, r); read_scale_one(next, t / 4 + 1, 1, r); }
-                }
-#pragma unroll
-                for (int r = e * PER_ASK; r < (e + 1) * PER_ASK; ++r) if (r < ASKS) ask_one(t + 3, (I + 3) % 4, FIRST + r);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            if constexpr (I == 3) now = next;
-        };
-        for (int t = 0; t < steps; t += 4) {
-            step(t, std::integral_constant<int, 0>());
-            if (t + 1 < steps) step(t + 1, std::integral_constant<int, 1>());
-            if (t + 2 < steps) step(t + 2, std::integral_constant<int, 2>());
-            if (t + 3 < steps) step(t + 3, std::integral_constant<int, 3>());
+            for (int i = 0; i < TN; ++i) o.w[h][i] = (int)((unsigned)o.w[h][i] >> 8);
         }
-        // (nothing is on its way to LDS or read there that the results would meet)
-        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    // in the order in which they are needed: w's first tile, a's, the others of w
+    auto in_order = [](int r) { return r == 0 ? TM : r <= TM ? r - 1 : r; };
+    // Keeps a matrix instruction where it is written: the branches of a step would otherwise have the compiler move all of them to its end.
+    auto stay = [](v16f &v) { asm volatile("" : "+a"(v)); };
+    constexpr int ALL = TM * TN, READS = TM + TN;
+    // Stores of a whole block by a wave.  Waits count what was issued behind what they wait for; vmcnt holds 63 at most.
+    constexpr int STORES = TM * TN * (Y == RNNT_TYPE_F32 ? 4 : 2), AHEAD = (STAGES - 3) * LOADS, AFTER = AHEAD + STORES < 63 ? AHEAD + STORES : 63;
+    static_assert(AHEAD < 63, "waits are counted");
+    Half half[2];
+    Scales now, next;
+    aim();
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) {
+        ask_scales();
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) ask_code(s, i);
+        advance();
     }
-    // Results leave by way of a wave's own part of LDS, 32 rows of y at a time, so that whole rows of the wave's columns are stored:
-    // register v of lane l holds row 8 (v / 4) + 4 (l / 32) + v % 4 of w's 32, row l % 32 of a's.  (Straight from the registers, sixteen
-    // bytes a row and store, this took 80 of 290 us of a product of 8192^3, for its stores and for fetching its code.)
-    constexpr int COLS = TN * 32, PITCH = COLS + 4, LANES = COLS / 4, ROWS = 64 / LANES;
-    static_assert(4 * 32 * PITCH * 4 <= S::LDS, "the waves' parts fit");
-    float *part = reinterpret_cast<float *>(lds) + wave * (32 * PITCH);
-    const int n = nb * S::BN + wn * COLS + lane % LANES * 4, left = g.N - n;
-    float bias[4];
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"((STAGES - 2) * LOADS) : "memory");
+    int stage = 0, group = 0;                              // of the step that comes; of the scales in `now`
+    read_scales(now, 0);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) bias[e] = g.bias && e < left ? g.bias[n + e] : 0.f;
-#pragma unroll
-    for (int j = 0; j < TM; ++j) {
-        asm volatile("" ::: "memory");
+    for (int i = 0; i < READS; ++i) read_one(half[0], 0, 0, i);
+    // Of the first steps of a block: whether there was none before it; whether STORES stores of the one before follow their pieces.
+    bool first = true, counted = false;
+#pragma clang loop unroll(disable)
+    for (int i_block = blockIdx.x >> 3; i_block < here; i_block += peers) {
+        v16f sum[TN][TM];
 #pragma unroll
         for (int i = 0; i < TN; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<v4f *>(part + (lane & 31) * PITCH + i * 32 + q * 8 + (lane >> 5) * 4) =
-                    v4f{sum[i][j][q * 4], sum[i][j][q * 4 + 1], sum[i][j][q * 4 + 2], sum[i][j][q * 4 + 3]};
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        const int m0 = mb * S::BM + wm * TM * 32 + j * 32, rows = min(32, g.M - m0);
-        if (left <= 0) continue;
-#pragma unroll 4
-        for (int r = lane / LANES; r < rows; r += ROWS) {
-            const v4f v = *reinterpret_cast<const v4f *>(part + r * PITCH + lane % LANES * 4);
-            const float o[4] = {v.x + bias[0], v.y + bias[1], v.z + bias[2], v.w + bias[3]};
-            store_four(g.y, g.y_type, (long long)(m0 + r) * g.y_stride + n, o, left);
+            for (int j = 0; j < TM; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum[i][j][e] = 0.f;
+#pragma clang loop unroll(disable)
+        for (int t = 0; t < steps; ++t) {
+            const int stage1 = stage + 1 == STAGES ? 0 : stage + 1, before = stage == 0 ? STAGES - 1 : stage - 1;
+            const bool rare = S::CHAIN && t < STAGES - 2 && !first, turn = t % 4 == 3 || t + 1 == steps;       // turn: the next step has other scales
+#pragma unroll
+            for (int e = 0; e < ALL; ++e) {
+                const int i = e / TM, j = e % TM;
+                sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(half[0].w[i]), operand(half[0].a[j]), sum[i][j], 4, 4, 0, now.w[0][i], 0, now.a[0][j]);
+                stay(sum[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int r = 0; r < READS; ++r) if (r * ALL / READS == e) read_one(half[1], stage, 1, in_order(r));
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // What step t + 1 needs is there; what was asked for later, and stores behind it, may still be on their way.
+            // (Stores of a block that is not whole are not counted: all of them are waited for.)
+            if (!rare) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(AHEAD) : "memory");
+            else if (counted) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(AFTER) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            asm volatile("s_barrier" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int e = 0; e < ALL; ++e) {
+                const int i = e / TM, j = e % TM;
+                sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(half[1].w[i]), operand(half[1].a[j]), sum[i][j], 4, 4, 0, now.w[1][i], 0, now.a[1][j]);
+                stay(sum[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int r = 0; r < READS; ++r) if (r * ALL / READS == e) read_one(half[0], stage1, 0, in_order(r));
+                if (e == 0) ask_scales();
+#pragma unroll
+                for (int r = 0; r < LOADS; ++r) if (1 + r * (ALL - 2) / LOADS == e) ask_code(before, r);
+                if (e == ALL / 2 && turn) read_scales(next, group + 1);
+                if (e == ALL - 1) advance();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            stage = stage1;
+            if (turn) { now = next; ++group; }
+            else shift(now);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        // Results leave by way of a wave's own part of LDS, 32 rows of 128 bytes of y at a time, so that lines are stored whole; 16-byte pieces are
+        // xored with the row.  Register v of lane l holds row 8 (v / 4) + 4 (l / 32) + v % 4 of w's 32, row l % 32 of a's.
+        // (Straight from the registers, sixteen bytes a row and store, this took 80 of 290 us of a product of 8192^3.)
+        constexpr int ACROSS = 128 / (32 * (int)sizeof(YT)), PIECE = 16 / (int)sizeof(YT);     // tiles of 32 columns, elements of 16 bytes
+        const Block k = block(i_block);
+        const int m0 = k.mb * S::BM + wm * TM * 32, n0 = k.nb * S::BN + wn * TN * 32;
+        const bool whole = m0 + TM * 32 <= g.M && n0 + TN * 32 <= g.N;
+        unsigned char *part = lds + (S::CHAIN ? STAGES * S::CODES + 2 * S::SCALES : 0) + wave * 4096;
+        // (without a place of their own: nothing is on its way to it or read there)
+        if constexpr (!S::CHAIN) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        int l = lane;
+        asm volatile("" : "+v"(l));                        // (places in y are worked out here, not before the steps, whose registers they would take)
+        const int row = l & 31, high = l >> 5, out_row = l >> 3, out_piece = l & 7;
+#pragma unroll
+        for (int i0 = 0; i0 < TN; i0 += ACROSS) {
+            // (the same for all lanes of a half: by way of the scalar cache, beside the loads that are counted)
+            float bias[ACROSS][4][4] = {};
+            const float *from_bias = g.bias + n0 + i0 * 32;
+            if (g.bias && whole) {
+#pragma unroll
+                for (int i = 0; i < ACROSS * 16; ++i) {
+                    const float low = from_bias[i / 4 * 8 + i % 4], up = from_bias[i / 4 * 8 + 4 + i % 4];
+                    bias[i / 16][i / 4 % 4][i % 4] = high ? up : low;
+                }
+            } else if (g.bias) {
+#pragma unroll
+                for (int i = 0; i < ACROSS * 16; ++i) bias[i / 16][i / 4 % 4][i % 4] = g.bias[min(n0 + i0 * 32 + i / 4 * 8 + high * 4 + i % 4, g.N - 1)];
+            }
+#pragma unroll
+            for (int j = 0; j < TM; ++j) {
+                wave_sync();
+#pragma unroll
+                for (int i = 0; i < ACROSS; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const v16f &from = sum[i0 + i][j];
+                        Piece<YT, 4> o;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o.e[e] = (YT)(from[q * 4 + e] + bias[i][q][e]);
+                        if constexpr (sizeof(YT) == 4) *reinterpret_cast<v4u *>(part + row * 128 + ((q * 2 + high) ^ (row & 7)) * 16) = __builtin_bit_cast(v4u, o);
+                        else *reinterpret_cast<unsigned long long *>(part + row * 128 + ((i * 4 + q) ^ (row & 7)) * 16 + high * 8) = __builtin_bit_cast(unsigned long long, o);
+                    }
+                wave_sync();
+                const int n = n0 + i0 * 32 + out_piece * PIECE;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int m = m0 + j * 32 + r * 8 + out_row;
+                    const unsigned char *piece = part + (r * 8 + out_row) * 128 + (out_piece ^ out_row) * 16;
+                    YT *to = static_cast<YT *>(g.y) + (long long)m * g.y_stride + n;
+                    if (whole) store_piece<YT, PIECE>(to, __builtin_bit_cast(Piece<YT, PIECE>, *reinterpret_cast<const v4u *>(piece)), PIECE);
+                    else if (m < g.M) {
+                        const int some = min(PIECE, g.N - n);
+#pragma unroll 1
+                        for (int e = 0; e < some; ++e) to[e] = reinterpret_cast<const YT *>(piece)[e];
+                    }
+                }
+            }
+        }
+        first = false;
+        counted = whole;
     }
+    // (nothing is on its way to LDS that is given up)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
 }  // namespace rnnt
@@ -474,11 +559,12 @@ uintptr_t size_of(int32_t type) { return type == RNNT_TYPE_F32 ? 4 : 2; }
 // Which kernel computes a product
 enum Plan { kDirect, kTiles128, kTiles256 };
 constexpr int64_t kDirectGroups = 256, kDirectRows = 512;
+constexpr int kComputeUnits = 256;     // of MI355X
 int64_t direct_groups(int64_t M, int64_t N, int nt) { return tiles(M, kTileRows) * tiles(tiles(N, kTileRows), nt); }
 Plan plan_of(int64_t M, int64_t N, int64_t K)
 {
     if (M <= kDirectRows || K == 0) return kDirect;
-    return tiles(M, 256) * tiles(N, 256) >= 256 ? kTiles256 : kTiles128;
+    return tiles(M, 256) * tiles(N, 256) >= 256 && K > kTileCols ? kTiles256 : kTiles128;
 }
 
 }  // namespace
@@ -570,16 +656,23 @@ int rnnt_mx4_product(const void *a, const void *a_scales, int32_t a_type, int64_
         args.a = to;
         args.a_scales = to + cb;
     }
-    auto run = [&](auto kernel, int bm, int bn, unsigned lds) -> int {
-        const int64_t mb = tiles(M, bm), nb = tiles(N, bn);
+    auto run = [&](auto shape, auto y) -> int {
+        typedef decltype(shape) S;
+        const auto kernel = mx4_tile_kernel<S, decltype(y)::value>;
+        const int64_t mb = tiles(M, S::BM), nb = tiles(N, S::BN);
         if (mb * nb > kMost / 8) return RNNT_ERR_UNSUPPORTED;
-        MX4_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(mb * nb)), dim3(256), lds, on, args, (int)mb, (int)nb);
+        MX4_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS));
+        const int64_t groups = S::CHAIN ? std::min<int64_t>(mb * nb, kComputeUnits * S::GROUPS) : mb * nb;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), S::LDS, on, args, (int)mb, (int)nb);
         MX4_TRY(hipGetLastError());
         return RNNT_OK;
     };
-    if (plan == kTiles256) return run(mx4_tile_kernel<4, 4>, 256, 256, TileShape<4, 4>::LDS);
-    return run(mx4_tile_kernel<2, 2>, 128, 128, TileShape<2, 2>::LDS);
+    auto with = [&](auto shape) -> int {
+        if (y_type == RNNT_TYPE_F32) return run(shape, std::integral_constant<int, RNNT_TYPE_F32>());
+        if (y_type == RNNT_TYPE_BF16) return run(shape, std::integral_constant<int, RNNT_TYPE_BF16>());
+        return run(shape, std::integral_constant<int, RNNT_TYPE_F16>());
+    };
+    return plan == kTiles256 ? with(TileShape<4, 4, 4, true>()) : with(TileShape<2, 2, 4, false>());
 }
 
 }  // extern "C"
