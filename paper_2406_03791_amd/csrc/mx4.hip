@@ -488,7 +488,7 @@ mx4_tile_kernel(const ProductArgs g, int m_blocks, int n_blocks)
         constexpr int ACROSS = 128 / (32 * (int)sizeof(YT)), PIECE = 16 / (int)sizeof(YT);     // tiles of 32 columns, elements of 16 bytes
         const Block k = block(i_block);
         const int m0 = k.mb * S::BM + wm * TM * 32, n0 = k.nb * S::BN + wn * TN * 32;
-        const bool whole = m0 + TM * 32 <= g.M && n0 + TN * 32 <= g.N;
+        const bool whole = (long long)m0 + TM * 32 <= g.M && (long long)n0 + TN * 32 <= g.N;
         unsigned char *part = lds + (S::CHAIN ? STAGES * S::CODES + 2 * S::SCALES : 0) + wave * 4096;
         // (without a place of their own: nothing is on its way to it or read there)
         if constexpr (!S::CHAIN) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
