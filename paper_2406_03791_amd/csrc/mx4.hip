@@ -25,6 +25,7 @@ template <int TYPE> struct Element;
 template <> struct Element<RNNT_TYPE_F32> { typedef float T; };
 template <> struct Element<RNNT_TYPE_BF16> { typedef __bf16 T; };
 template <> struct Element<RNNT_TYPE_F16> { typedef _Float16 T; };
+template <> struct Element<RNNT_TYPE_MX4> { typedef unsigned char T; };
 
 // The biased exponent k + 127 of a block whose largest magnitude has these bits: the smallest k with top <= 1.5 * 2^(k + 2).
 // (Adding 0x3fffff carries into the exponent where the mantissa is above 1.5; below 2^-126 there is only -127.)
@@ -219,44 +220,61 @@ struct ProductArgs {
 
 __device__ __forceinline__ v8i operand(const v4u &c) { return v8i{(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0}; }
 
-// Few rows: latency bound.  A work-group computes 16 rows of a by 16 NT rows of w; its four waves take every fourth tile
-// of K each and add up at the end.  Operands go from memory to registers: a lane's part of a tile is a row's block, 32 values,
-// which it quantises by itself.
-template <int A, int NT>
-__global__ void __launch_bounds__(256)
+// Few rows: bound by latency, and for large w by reading it.  A work-group computes 16 rows of a by 16 NT rows of w; its WAVES waves
+// take the tiles of K in turn and add up at the end.  Operands go from memory to registers: a lane's part of a tile is a row's
+// block, 32 values, which it quantises by itself.  Two shapes: eight waves by 32 rows of w, and, from 256 work-groups of it on, four by 64, with
+// half as many readers of a.  us, bf16, first shape and second: 16 x 8192 x 8192 12.3 and 15.6, 128 x 4096 x 1024 8.2 and 5.8.
+// (Tiles asked for ahead, two to four: 4.4 to 4.8 in place of 4.0 for small ones, nothing gained for large ones.)
+template <int A, int NT, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64)
 mx4_product_kernel(const ProductArgs g)
 {
-    constexpr int PITCH = NT * 16 + 4;
-    __shared__ __align__(16) float sums[4][16 * PITCH];
+    typedef typename Element<A>::T T;                      // (of codes: bytes, 16 of them)
+    constexpr int PITCH = NT * 16 + 4, PER = 16 / (int)sizeof(T), PIECES = A == RNNT_TYPE_MX4 ? 1 : RNNT_MX4_BLOCK / PER;
+    __shared__ __align__(16) float sums[WAVES][16 * PITCH];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r = lane & 15, b = lane >> 4;
     const int steps = (int)tiles(g.K, kTileCols), groups = (int)tiles(g.K, kScaleCols), n_tiles = (int)tiles(g.N, kTileRows);
     const int across = (int)tiles(n_tiles, NT), mt = blockIdx.x / across, nt = (blockIdx.x - mt * across) * NT;
-    const long long row = (long long)mt * kTileRows + r;
-    v4f sum[NT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) sum[i] = v4f{0.f, 0.f, 0.f, 0.f};
-    for (int s = wave; s < steps; s += 4) {
-        v4u wc[NT], ac;
-        unsigned ws[NT], as;
+    // (a row beyond the last one repeats it and is not stored)
+    const T *row = static_cast<const T *>(g.a) + (A == RNNT_TYPE_MX4 ? (long long)mt * steps * kTileBytes + lane * 16
+                                                                   : min((long long)mt * kTileRows + r, (long long)g.M - 1) * g.a_stride + b * RNNT_MX4_BLOCK);
+    struct Tile { v4u w[NT]; Piece<T, PER> a[PIECES]; unsigned ws[NT], as; };
+    auto load = [&](Tile &o, int s) {
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
             const long long t = min(nt + i, n_tiles - 1);
-            wc[i] = *reinterpret_cast<const v4u *>(g.w + (t * steps + s) * kTileBytes + lane * 16);
-            ws[i] = g.w_scales[(t * groups + s / 4) * kScaleBytes + lane * 4 + (s & 3)];
+            o.w[i] = *reinterpret_cast<const v4u *>(g.w + (t * steps + s) * kTileBytes + lane * 16);
+            o.ws[i] = g.w_scales[(t * groups + s / 4) * kScaleBytes + lane * 4 + (s & 3)];
         }
         if constexpr (A == RNNT_TYPE_MX4) {
-            ac = *reinterpret_cast<const v4u *>(static_cast<const unsigned char *>(g.a) + ((long long)mt * steps + s) * kTileBytes + lane * 16);
-            as = g.a_scales[((long long)mt * groups + s / 4) * kScaleBytes + lane * 4 + (s & 3)];
+            o.a[0] = load_piece<T, PER>(row + (long long)s * kTileBytes, PER);
+            o.as = g.a_scales[((long long)mt * groups + s / 4) * kScaleBytes + lane * 4 + (s & 3)];
+        } else if ((s + 1) * kTileCols <= g.K) {           // (the same for all lanes)
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) o.a[i] = load_piece<T, PER>(row + s * kTileCols + i * PER, PER);
         } else {
-            typedef typename Element<A>::T T;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) o.a[i] = load_piece<T, PER>(row + s * kTileCols + i * PER, g.K - s * kTileCols - b * RNNT_MX4_BLOCK - i * PER);
+        }
+    };
+    v4f sum[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) sum[i] = v4f{0.f, 0.f, 0.f, 0.f};
+    for (int s = wave; s < steps; s += WAVES) {
+        Tile t;
+        load(t, s);
+        v4u c;
+        unsigned scale;
+        if constexpr (A == RNNT_TYPE_MX4) { c = __builtin_bit_cast(v4u, t.a[0]); scale = t.as; }
+        else {
             float v[32];
-            const int col = s * kTileCols + b * RNNT_MX4_BLOCK;
-            load_block<T>(v, static_cast<const T *>(g.a) + row * g.a_stride + col, row < g.M ? g.K - col : 0);
-            ac = quantize_block(v, as);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = (float)t.a[i / PER].e[i % PER];
+            c = quantize_block(v, scale);
         }
 #pragma unroll
         for (int i = 0; i < NT; ++i)
-            sum[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(wc[i]), operand(ac), sum[i], 4, 4, 0, (int)ws[i], 0, (int)as);
+            sum[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(t.w[i]), operand(c), sum[i], 4, 4, 0, (int)t.ws[i], 0, (int)scale);
     }
     // (a lane holds four neighbours of w's rows for one of a's)
 #pragma unroll
@@ -270,7 +288,14 @@ mx4_product_kernel(const ProductArgs g)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const int at = m * PITCH + c + e;
-        o[e] = ((sums[0][at] + sums[1][at]) + (sums[2][at] + sums[3][at])) + (g.bias && n + e < g.N ? g.bias[n + e] : 0.f);
+        float all[WAVES];
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) all[i] = sums[i][at];
+#pragma unroll
+        for (int half = WAVES / 2; half > 0; half /= 2)
+#pragma unroll
+            for (int i = 0; i < half; ++i) all[i] += all[i + half];
+        o[e] = all[0] + (g.bias && n + e < g.N ? g.bias[n + e] : 0.f);
     }
     store_four(g.y, g.y_type, ((long long)mt * kTileRows + m) * g.y_stride + n, o, g.N - n);
 }
@@ -566,15 +591,21 @@ bool is_number(int32_t type) { return type == RNNT_TYPE_F32 || type == RNNT_TYPE
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 uintptr_t size_of(int32_t type) { return type == RNNT_TYPE_F32 ? 4 : 2; }
 
-// Which kernel computes a product
+// Which kernel computes a product.  The one for few rows takes 3.5 us and one more for every 2 * 10^8 of M N K (of codes twice
+// that); tiles (and the quantisation before them) take 10 us, up to K = 8192 25, before their size shows (of codes 7 and 20).
+// us, few rows and tiles, of bf16: 256 x 4096 x 1024 9.2 and 10.8, 2048 x 1030 x 640 13.3 and 11.7, 128 x 4096 x 4096 13.6 and 17.5,
+// 256 x 4096 x 4096 25.6 and 18.2, 64 x 8192 x 8192 24.9 and 28.4, 128 x 8192 x 8192 45.4 and 28.8; of codes: 256 x 4096 x 4096 12.2 and 13.8,
+// 128 x 8192 x 8192 21.1 and 23.9.  Blocks of 256 x 256 where there is one for every compute unit (and two steps of K, which their
+// pipeline is made for): 8192 x 8192 x 1024 62 us, by 128 x 128 71; 4096^3 42, by 128 x 128 45.
 enum Plan { kDirect, kTiles128, kTiles256 };
-constexpr int64_t kDirectGroups = 256, kDirectRows = 512;
+constexpr int64_t kDirectGroups = 256;
+constexpr double kDirectWork = 1 << 28;
 constexpr int kComputeUnits = 256;     // of MI355X
 int64_t direct_groups(int64_t M, int64_t N, int nt) { return tiles(M, kTileRows) * tiles(tiles(N, kTileRows), nt); }
-Plan plan_of(int64_t M, int64_t N, int64_t K)
+Plan plan_of(int32_t a_type, int64_t M, int64_t N, int64_t K)
 {
-    if (M <= kDirectRows || K == 0) return kDirect;
-    return tiles(M, 256) * tiles(N, 256) >= 256 && K > kTileCols ? kTiles256 : kTiles128;
+    if ((double)M * (double)N * (double)K <= kDirectWork * (3 + K / kScaleCols) * (a_type == RNNT_TYPE_MX4 ? 1.5 : 1.0)) return kDirect;
+    return tiles(M, 256) * tiles(N, 256) >= kComputeUnits && K > kTileCols ? kTiles256 : kTiles128;
 }
 
 }  // namespace
@@ -624,7 +655,7 @@ int rnnt_mx4_product_workspace(int32_t a_type, int64_t M, int64_t N, int64_t K, 
     if ((!is_number(a_type) && a_type != RNNT_TYPE_MX4) || M < 0 || N < 0 || K < 0) return RNNT_ERR_SHAPE;
     if (M > kMost || N > kMost || K > kMost) return RNNT_ERR_UNSUPPORTED;
     int64_t codes = 0, scales = 0;
-    if (a_type != RNNT_TYPE_MX4 && plan_of(M, N, K) != kDirect) (void)rnnt_mx4_sizes(M, K, &codes, &scales);
+    if (a_type != RNNT_TYPE_MX4 && plan_of(a_type, M, N, K) != kDirect) (void)rnnt_mx4_sizes(M, K, &codes, &scales);
     *bytes_out = codes + scales;
     return RNNT_OK;
 }
@@ -646,15 +677,15 @@ int rnnt_mx4_product(const void *a, const void *a_scales, int32_t a_type, int64_
     const hipStream_t on = static_cast<hipStream_t>(stream);
     ProductArgs args{a, static_cast<const unsigned char *>(a_scales), static_cast<const unsigned char *>(w_codes), static_cast<const unsigned char *>(w_scales),
                      bias, y, a_stride, y_stride, y_type, (int)M, (int)N, (int)K};
-    const Plan plan = plan_of(M, N, K);
+    const Plan plan = plan_of(a_type, M, N, K);
     if (plan == kDirect) {
-        const int nt = direct_groups(M, N, 4) >= kDirectGroups ? 4 : 1;
+        const int nt = direct_groups(M, N, 4) >= kDirectGroups ? 4 : 2;
         const int64_t blocks = direct_groups(M, N, nt);
         if (blocks > kMost) return RNNT_ERR_UNSUPPORTED;
-        auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, on, args); };
-        auto with = [&](auto type) {
-            constexpr int A = decltype(type)::value;
-            if (nt == 4) run(mx4_product_kernel<A, 4>); else run(mx4_product_kernel<A, 1>);
+        auto run = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(waves * 64), 0, on, args); };
+        auto with = [&](auto t) {
+            if (nt == 4) run(mx4_product_kernel<t(), 4, 4>, 4);
+            else run(mx4_product_kernel<t(), 2, 8>, 8);
         };
         if (a_type == RNNT_TYPE_F32) with(std::integral_constant<int, RNNT_TYPE_F32>());
         else if (a_type == RNNT_TYPE_BF16) with(std::integral_constant<int, RNNT_TYPE_BF16>());

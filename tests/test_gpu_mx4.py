@@ -110,7 +110,8 @@ def _check_product(got, qa, qw, bias, y_type, K):
 
 
 SHAPES = [(1, 1, 1), (1, 17, 32), (3, 5, 33), (8, 1025, 640), (16, 16, 128), (17, 33, 129), (33, 257, 511), (64, 130, 512), (70, 65, 700),
-          (130, 96, 1024), (257, 300, 96), (300, 513, 1500), (31, 48, 2560), (512, 384, 640), (1030, 272, 160), (2100, 640, 1024)]
+          (130, 96, 1024), (257, 300, 96), (300, 513, 1500), (31, 48, 2560), (512, 384, 640), (1030, 272, 160), (2100, 640, 1024),
+          (1500, 1300, 1100), (700, 3001, 1000), (3000, 333, 2000), (5, 4097, 1000), (20, 300, 9000)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
@@ -159,7 +160,7 @@ def test_large_products(pkg, M, N, K, a_type, y_type):  # noqa: F811
 def test_what_is_not_finite_stays_in_its_row_and_column(pkg, M, a_type):  # noqa: F811
     import torch
     g = torch.Generator().manual_seed(M)
-    N, K = 200, 300
+    N, K = (200, 300) if M < 2000 else (1700, 800)
     a, w = torch.randn((M, K), generator=g), torch.randn((N, K), generator=g)
     a[2, 299], a[M - 1, 5], w[7, 64], w[199, 299] = float("nan"), float("inf"), float("-inf"), float("nan")
     if a_type == "bf16":
