@@ -354,12 +354,10 @@ template <int WIDTH> struct Joined {
 // LDS of a work-group that joins: the waves' buffers or their lists, which take turns, and the tokens
 __host__ __device__ constexpr size_t join_lds(int waves, int beams, int n) { return (size_t)waves * kBuffer * 8 + (size_t)beams * n * 4; }
 
-// A work-group an utterance, its waves take the hypotheses in turn
+// The hypotheses of an utterance by a work-group, whose waves take them in turn
 template <int TYPE, int WIDTH>
-__global__ void __launch_bounds__(kJoinWaves * 64)
-beam_select_kernel(const SelectArgs a)
+__device__ __forceinline__ void select_rows(const SelectArgs &a, unsigned char *lds)
 {
-    extern __shared__ __align__(16) unsigned char lds[];
     const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), b = blockIdx.x;
     u64 *buffers = reinterpret_cast<u64 *>(lds);
     Joined<WIDTH> all{a, reinterpret_cast<int *>(buffers + waves * kBuffer), (int)threadIdx.x & 63};
@@ -374,6 +372,152 @@ beam_select_kernel(const SelectArgs a)
     }
     __syncthreads();
     all.finish(b, wave, waves, buffers, reinterpret_cast<unsigned *>(buffers + waves * 64));
+}
+template <int TYPE, int WIDTH>
+__global__ void __launch_bounds__(kJoinWaves * 64)
+beam_select_kernel(const SelectArgs a)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    select_rows<TYPE, WIDTH>(a, lds);
+}
+
+// Short rows (a tile and a last lane each), a wave a row, few winners: no lists.  The lanes' largest candidates over all rows are 64 different
+// ones; the n-th of those bounds the n-th best of the utterance from below, and what is not below the bound, for n = 16 about
+// 18 candidates of independent logits, is put together in LDS and ranked by counting.  Where ties make more than
+// kShort of them, the utterance is done by lists.  bf16, with lists in brackets: 128 utterances of 16 rows of 1025 for 16 winners
+// 8.6 us (12.0), of 4 rows for 4 5.3 (6.5); 2048 of 8 rows for 8 25 (33); 2048 of 16 rows of 128 for 16 53 (76).  Every wave counts for itself where
+// the bound is, which one or two rows do not repay: 4096 of one row of 1025 for 16 15.2 (11.5), 128 of two 7.5 (7.4).
+constexpr int kShort = 64, kShortWinners = 16, kShortRows = 3, kShortRow = kTile + 64;
+struct Candidate {
+    u64 key, sub;          // the score's place in the order of doubles; hypothesis (complement), logit's place, token (complement)
+    __device__ __forceinline__ bool above(const Candidate &o) const { return key > o.key || (key == o.key && sub > o.sub); }
+};
+struct ShortLds { unsigned group[64]; Candidate found[kShort]; int count; };
+
+__device__ __forceinline__ unsigned float_key(float f)      // (more than 0, which is nothing)
+{
+    const unsigned u = __float_as_uint(f);
+    return u >> 31 ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float key_float(unsigned u) { return u >> 31 ? __uint_as_float(u ^ 0x80000000u) : u ? __uint_as_float(~u) : -INFINITY; }
+
+__device__ __forceinline__ u64 score_key(double t)
+{
+    const u64 u = __builtin_bit_cast(u64, t + 0.0);
+    return t > -INFINITY ? (u >> 63 ? ~u : u | 0x8000000000000000ull) : 0;
+}
+
+template <int TYPE>
+__global__ void __launch_bounds__(kJoinWaves * 64)
+beam_short_kernel(const SelectArgs a)
+{
+    typedef typename Logit<TYPE>::T T;
+    constexpr int PER = 16 / (int)sizeof(T), LOADS = kTile / 64 / PER, ALL = kTile / 64 + 1;
+    struct __attribute__((packed, aligned(sizeof(T)))) At { T e[PER]; };
+    extern __shared__ __align__(16) unsigned char lds[];
+    ShortLds &s = *reinterpret_cast<ShortLds *>(lds);
+    const int waves = blockDim.x >> 6, k = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, b = blockIdx.x, n = a.n_out;
+    const bool has_row = k < a.beams, full = a.V >= kTile;
+    const long long hyp = (long long)b * a.beams + (has_row ? k : 0);
+    const T *row = static_cast<const T *>(a.logits) + b * a.batch_stride + (has_row ? k : 0) * a.beam_stride;
+    // the row's logits, 17 a lane; `place`: where in the row
+    float f[ALL];
+    if (full) {
+        At v[LOADS];
+#pragma unroll
+        for (int q = 0; q < LOADS; ++q) v[q] = *reinterpret_cast<const At *>(row + (q * 64 + lane) * PER);
+        const T more = row[min(kTile + lane, a.V - 1)];
+#pragma unroll
+        for (int i = 0; i < ALL - 1; ++i) f[i] = (float)v[i / PER].e[i % PER];
+        f[ALL - 1] = kTile + lane < a.V ? (float)more : -INFINITY;
+    } else {
+        T v[ALL - 1];
+#pragma unroll
+        for (int i = 0; i < ALL - 1; ++i) v[i] = row[min(i * 64 + lane, a.V - 1)];
+#pragma unroll
+        for (int i = 0; i < ALL - 1; ++i) f[i] = i * 64 + lane < a.V ? (float)v[i] : -INFINITY;
+        f[ALL - 1] = -INFINITY;
+    }
+    auto place = [&](int i) { return !full ? i * 64 + lane : i < ALL - 1 ? (i / PER * 64 + lane) * PER + i % PER : kTile + lane; };
+    const float score = a.scores[hyp];
+    const bool ended = has_row && a.finished && a.finished[hyp], live = has_row && !ended && score > -INFINITY;
+    if (k == 0) { s.group[lane] = 0; if (lane == 0) s.count = 0; }
+    float m = f[0];
+#pragma unroll
+    for (int i = 1; i < ALL; ++i) m = fmaxf(m, f[i]);
+    const float top = fmaxf(wave_max(m), kLowest);
+    // (differences to the largest logit: at the ends of the type, too)
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < ALL; ++i) part[i % 4] += __builtin_amdgcn_exp2f((f[i] - top) * kLog2E);
+    const double sum = wave_sum((double)((part[0] + part[1]) + (part[2] + part[3])));
+    const double base = (double)score - log(sum);          // (NaN where the row holds a NaN or an infinity)
+    auto total = [&](float x) { return base + ((double)x - (double)top); };
+    __syncthreads();                                       // (the cleared LDS)
+    if (live && m > -INFINITY) {
+        const double t = total(m);
+        if (t > -INFINITY) atomicMax(&s.group[lane], float_key((float)t));
+    }
+    __syncthreads();
+    // the n-th of the lanes' largest
+    const unsigned best = s.group[lane];
+    unsigned nth = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 8; --bit) {
+        const unsigned with = nth | 1u << bit;
+        if (__popcll(__ballot(best >= with)) >= n) nth = with;
+    }
+    const float bar = key_float(nth);
+    // In the row's logits, and lower by more than all these roundings are off: logits from there on are candidates.
+    const double at = (double)bar - base + (double)top;
+    const float low = at == at ? (float)(at - (fabs(at) + fabs((double)bar) + fabs((double)top)) * 1e-6 - 1e-5) : -INFINITY;
+    u64 in[ALL];
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < ALL; ++i) { in[i] = live && base == base ? __ballot(f[i] >= low && f[i] > -INFINITY) : 0; mine += __popcll(in[i]); }
+    if (ended) mine = 1;
+    if (mine > 0) {
+        int from = 0;
+        if (lane == 0) from = atomicAdd(&s.count, mine);
+        from = __builtin_amdgcn_readfirstlane(from);
+        auto put = [&](float x, int token, double t, int to) {
+            if (to < kShort) s.found[to] = Candidate{score_key(t), (u64)(63 - k) << 58 | (row_key(x, 0) >> 32) << 26 | (u64)(0x3ffffff - token)};
+        };
+        if (ended) { if (lane == 0) put(0.f, a.end_token, (double)score, from); }
+        else {
+#pragma unroll
+            for (int i = 0; i < ALL; ++i) {
+                if (in[i] == 0ull) continue;
+                if (in[i] >> lane & 1) put(f[i], place(i), total(f[i]), from + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(in[i] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)in[i], 0u)));
+                from += __popcll(in[i]);
+            }
+        }
+    }
+    __syncthreads();
+    const int count = s.count;
+    if (count > kShort) {                                  // (the whole work-group)
+        __syncthreads();
+        select_rows<TYPE, 16>(a, lds);
+        return;
+    }
+    // a wave ranks every waves-th candidate: how many are above it
+    const Candidate own = lane < count ? s.found[lane] : Candidate{0, 0};
+    for (int c = k; c < count; c += waves) {
+        const Candidate it = s.found[c];
+        const int rank = __popcll(__ballot(own.above(it)));
+        if (lane == 0 && rank < n && it.key != 0) {
+            const long long o = (long long)b * n + rank;
+            const u64 u = it.key >> 63 ? it.key ^ 0x8000000000000000ull : ~it.key;
+            a.scores_out[o] = (float)__builtin_bit_cast(double, u);
+            a.tokens_out[o] = 0x3ffffff - (int)(it.sub & 0x3ffffff);
+            a.parents_out[o] = 63 - (int)(it.sub >> 58);
+        }
+    }
+    const int there = __popcll(__ballot(own.key != 0));
+    if (k == 0 && lane >= there && lane < n) {
+        const long long o = (long long)b * n + lane;
+        a.scores_out[o] = -INFINITY; a.tokens_out[o] = -1; a.parents_out[o] = -1;
+    }
 }
 
 // Few utterances with long rows: pieces over the whole device, joined by a second launch.  A work-group's waves have four pieces
@@ -582,7 +726,7 @@ bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(
 constexpr int kOneLaunchTiles = 8, kWavesWanted = 4096;
 
 struct SelectPlan {
-    bool two = false;
+    bool two = false, is_short = false;
     int pieces = 1, piece_tiles = 1, waves = 1;
     size_t lds = 0;
     int64_t bytes = 0;
@@ -590,7 +734,8 @@ struct SelectPlan {
     {
         const int row = (V - 1) / kTile + 1;
         while (waves < kJoinWaves && waves < beams) waves *= 2;
-        lds = join_lds(waves, beams, n);
+        is_short = V <= kShortRow && beams >= kShortRows && beams <= kJoinWaves && n <= kShortWinners;
+        lds = std::max(join_lds(waves, beams, n), is_short ? sizeof(ShortLds) : 0);
         if ((beams + waves - 1) / waves * row <= kOneLaunchTiles || B * beams >= kWavesWanted) return;
         two = true;
         const int64_t into = std::min<int64_t>(std::max<int64_t>(kWavesWanted / (B * beams * kScanWaves), 1), std::min(64 / kScanWaves, (row + 2 * kScanWaves - 1) / (2 * kScanWaves)));
@@ -634,7 +779,11 @@ int rnnt_beam_select(const void *logits, int32_t type, int64_t batch_stride, int
     const hipStream_t on = static_cast<hipStream_t>(stream);
     if (!p.two) {
         auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(B), dim3(p.waves * 64), (unsigned)p.lds, on, args); };
-        auto with = [&](auto t) { if (n_out <= 16) run(beam_select_kernel<t(), 16>); else run(beam_select_kernel<t(), 64>); };
+        auto with = [&](auto t) {
+            if (p.is_short) run(beam_short_kernel<t()>);
+            else if (n_out <= 16) run(beam_select_kernel<t(), 16>);
+            else run(beam_select_kernel<t(), 64>);
+        };
         if (type == RNNT_TYPE_F32) with(std::integral_constant<int, RNNT_TYPE_F32>());
         else if (type == RNNT_TYPE_BF16) with(std::integral_constant<int, RNNT_TYPE_BF16>());
         else with(std::integral_constant<int, RNNT_TYPE_F16>());

@@ -71,6 +71,36 @@ def test_ties_go_to_the_lowest_place(pkg, V, n):  # noqa: F811
         _check(pkg, x.contiguous(), torch.zeros((1, 3)), n)
 
 
+@pytest.mark.parametrize("B,beams,V,n", [(2, 3, 1, 2), (3, 16, 1, 16), (2, 4, 63, 16), (3, 7, 1023, 11), (3, 16, 1024, 16), (2, 5, 1025, 1), (2, 16, 1087, 16),
+                                         (2, 15, 1088, 16), (2, 16, 1089, 16), (2, 16, 1025, 17), (2, 17, 1025, 16), (300, 3, 40, 5)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_short_rows(pkg, B, beams, V, n, dtype):  # noqa: F811
+    """Around the lengths, hypotheses and winners up to which rows are short: random logits, few different ones, all the
+    same but a few, masked ones, and magnitudes at which the scores lose the logits."""
+    import torch
+    g = torch.Generator().manual_seed(B + 10 * beams + V + n)
+    scores = -torch.rand((B, beams), generator=g) * 8
+    finished = torch.rand((B, beams), generator=g) < 0.3
+    plain = torch.randn((B, beams, V), generator=g) * 2
+    masked = plain.masked_fill(torch.rand((B, beams, V), generator=g) < 0.95, -float("inf"))
+    masked[0, 1], masked[0, 2, V // 2], masked[B - 1] = -float("inf"), float("nan"), -float("inf")
+    few = torch.randint(0, 3, (B, beams, V), generator=g).float()
+    same = torch.zeros((B, beams, V))
+    same[:, :, ::97] = 1
+    peaks = plain.clone()
+    peaks[:, 1, V - 1] += 30
+    for x in (plain, masked, few, same, peaks, plain * 1e4):
+        x = x.to(_torch_type(dtype))
+        _check(pkg, x, scores, n)
+        _check(pkg, x, scores, n, finished, end=V - 1)
+    x = few.to(_torch_type(dtype))
+    _check(pkg, x, torch.zeros((B, beams)), n)
+    _check(pkg, x, scores * 1e4, n)
+    far = scores.clone()
+    far[:, 0], far[:, 2], far[0, 1] = -1e30, -1e38, -float("inf")
+    _check(pkg, x, far, n)
+
+
 def test_zeros_of_either_sign_tie(pkg):  # noqa: F811
     import torch
     x = torch.full((1, 1, 100), -1.0)
