@@ -249,7 +249,7 @@ mx4_product_kernel(const ProductArgs g)
         if constexpr (A == RNNT_TYPE_MX4) {
             o.a[0] = load_piece<T, PER>(row + (long long)s * kTileBytes, PER);
             o.as = g.a_scales[((long long)mt * groups + s / 4) * kScaleBytes + lane * 4 + (s & 3)];
-        } else if ((s + 1) * kTileCols <= g.K) {           // (the same for all lanes)
+        } else if ((long long)(s + 1) * kTileCols <= g.K) {        // (the same for all lanes)
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) o.a[i] = load_piece<T, PER>(row + s * kTileCols + i * PER, PER);
         } else {
