@@ -667,7 +667,7 @@ int rnnt_beam_select(const void *logits, int32_t type, int64_t batch_stride, int
  * writes it: where it is outside [0, beams_in) the row becomes zeros.  dst may be src
  * (with the same strides and beams_in = beams_out); otherwise no destination row may overlap
  * a source row or another destination row.  1 <= beams_in, beams_out <= 64, 1 <= n_states <=
- * RNNT_BEAM_STATES, negative counts or strides, destination rows closer than row_bytes:
+ * RNNT_BEAM_STATES, negative counts or strides, destination rows (of o, b or j) closer than row_bytes:
  * RNNT_ERR_SHAPE.  `states` is a HOST array, read within the call.  B = 0: nothing is done.
  */
 #define RNNT_BEAM_STATES 16

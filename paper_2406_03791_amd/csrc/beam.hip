@@ -825,7 +825,7 @@ int rnnt_beam_reorder(const rnnt_beam_state *states, int32_t n_states, const int
         const rnnt_beam_state &s = states[i];
         if (s.outer < 0 || s.row_bytes < 0 || s.src_outer < 0 || s.src_batch < 0 || s.src_beam < 0 || s.dst_outer < 0 || s.dst_batch < 0 || s.dst_beam < 0)
             return RNNT_ERR_SHAPE;
-        if (beams_out > 1 && s.dst_beam < s.row_bytes) return RNNT_ERR_SHAPE;
+        if ((beams_out > 1 && s.dst_beam < s.row_bytes) || (B > 1 && s.dst_batch < s.row_bytes) || (s.outer > 1 && s.dst_outer < s.row_bytes)) return RNNT_ERR_SHAPE;
         if (s.src == s.dst && s.src && (beams_in != beams_out || s.src_outer != s.dst_outer || s.src_batch != s.dst_batch || s.src_beam != s.dst_beam))
             return RNNT_ERR_SHAPE;
         if (B == 0 || s.outer == 0 || s.row_bytes == 0) continue;

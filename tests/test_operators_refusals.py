@@ -99,6 +99,8 @@ def test_reorder(lib):
     assert f(k_in=0) == SHAPE and f(k_in=65) == SHAPE and f(k_out=0) == SHAPE and f(k_out=65) == SHAPE
     for k in ("outer", "row_bytes", "src_outer", "src_batch", "src_beam", "dst_outer", "dst_batch", "dst_beam"):
         assert f(**{k: -1}) == SHAPE
-    assert f(dst_beam=63) == SHAPE
+    assert f(dst_beam=63) == SHAPE and f(dst_batch=63) == SHAPE and f(dst_outer=63) == SHAPE and f(dst_batch=0) == SHAPE
+    assert f(dst=P, src_batch=0, dst_batch=0) == SHAPE and f(dst=P, src_outer=0, dst_outer=0) == SHAPE
+    assert f(B=0, dst_batch=0) == OK and f(outer=0, dst_outer=0) == OK
     assert f(dst=P, k_out=3) == SHAPE and f(dst=P, dst_batch=512) == SHAPE       # within itself: the same strides and beams
     assert f(outer=2 ** 31) == UNSUPPORTED
