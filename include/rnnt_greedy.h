@@ -572,7 +572,8 @@ int rnnt_probe_mfma(int32_t shape, double *tflops_out);
  * nothing, reads nothing back, keeps nothing for the next call, and may be
  * captured into a graph.  Errors are found on the host before anything is queued.
  * Calls may overlap as long as they share no output and no workspace.  Outputs
- * are the same bits from call to call on the same inputs.
+ * are the same bits from call to call on the same inputs.  What would take 2^32 or
+ * more threads is refused (RNNT_ERR_UNSUPPORTED).
  *
  * Types of tensors; strides and the counts of rows and columns are in elements,
  * and a tensor's address is a multiple of its element's size (RNNT_ERR_SHAPE).

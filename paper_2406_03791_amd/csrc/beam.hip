@@ -718,6 +718,7 @@ namespace {
         if (e_ != hipSuccess) return hip_fail(e_, #expr);       \
     } while (0)
 
+constexpr int64_t kMostThreads = 0xffffffff;                                // of a launch, at most
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 // How a selection is cut up.  One launch, a work-group an utterance and a wave a row, where that leaves a wave no more than
@@ -774,6 +775,7 @@ int rnnt_beam_select(const void *logits, int32_t type, int64_t batch_stride, int
         !aligned(parents_out, 4)) return RNNT_ERR_SHAPE;
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return RNNT_ERR_SCRATCH;
     const SelectPlan p(B, beams, V, n_out);
+    if ((int64_t)B * p.waves * 64 > kMostThreads) return RNNT_ERR_UNSUPPORTED;
     SelectArgs args{logits, scores, finished, scores_out, tokens_out, parents_out, batch_stride, beam_stride, B, beams, V, n_out, end_token,
                     p.pieces, p.piece_tiles, nullptr, nullptr, nullptr};
     const hipStream_t on = static_cast<hipStream_t>(stream);
@@ -791,7 +793,7 @@ int rnnt_beam_select(const void *logits, int32_t type, int64_t batch_stride, int
         return RNNT_OK;
     }
     const int64_t n = (int64_t)B * beams * p.pieces;
-    if (n > 0x7fffffff) return RNNT_ERR_UNSUPPORTED;
+    if (n * kScanWaves * 64 > kMostThreads) return RNNT_ERR_UNSUPPORTED;
     args.lists = static_cast<u64 *>(workspace);
     args.sums = reinterpret_cast<double *>(args.lists + n * n_out);
     args.refs = args.sums + n * kScanWaves;
@@ -845,7 +847,7 @@ int rnnt_beam_reorder(const rnnt_beam_state *states, int32_t n_states, const int
         any_within = any_within || within;
         bytes += (double)s.row_bytes * beams_out * s.outer * B;
         groups += chunks * s.outer * B;
-        if (groups > 0x7fffffff) return RNNT_ERR_UNSUPPORTED;
+        if (groups * 256 > kMostThreads) return RNNT_ERR_UNSUPPORTED;
     }
     if (args.n == 0) return RNNT_OK;
     auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, static_cast<hipStream_t>(stream), args); };

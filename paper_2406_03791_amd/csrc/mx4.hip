@@ -92,19 +92,6 @@ __device__ __forceinline__ void store_piece(T *p, const Piece<T, N> &v, long lon
     }
 }
 
-// The block of 32 values at p of a row that goes on for `left` values from there
-template <class T>
-__device__ __forceinline__ void load_block(float (&v)[32], const T *p, long long left)
-{
-    constexpr int PER = 16 / sizeof(T);
-#pragma unroll
-    for (int i = 0; i < 32 / PER; ++i) {
-        const Piece<T, PER> a = load_piece<T, PER>(p + i * PER, left - i * PER);
-#pragma unroll
-        for (int e = 0; e < PER; ++e) v[i * PER + e] = (float)a.e[e];
-    }
-}
-
 // The largest of the lanes that hold a block: 8 or 4 neighbours.
 template <int LANES>
 __device__ __forceinline__ unsigned block_top(unsigned m)
@@ -584,7 +571,7 @@ namespace {
         if (e_ != hipSuccess) return hip_fail(e_, #expr);       \
     } while (0)
 
-constexpr int64_t kMost = 0x7fffffff;
+constexpr int64_t kMost = 0x7fffffff, kMostThreads = 0xffffffff;          // rows or columns; threads of a launch
 constexpr int64_t kStreamValues = 8 << 20;    // floats that the L2s of the eight XCDs hold together
 
 bool is_number(int32_t type) { return type == RNNT_TYPE_F32 || type == RNNT_TYPE_BF16 || type == RNNT_TYPE_F16; }
@@ -632,7 +619,7 @@ int rnnt_mx4_quantize(const void *x, int32_t type, int64_t rows, int64_t cols, i
     if (!aligned(x, size_of(type)) || !aligned(codes_out, 16) || !aligned(scales_out, 16) || !aligned(values_out, 4)) return RNNT_ERR_SHAPE;
     const int ct = (int)tiles(cols, kTileCols), st = (int)tiles(cols, kScaleCols);
     const long long blocks = tiles(rows, kTileRows) * st;
-    if (blocks > kMost) return RNNT_ERR_UNSUPPORTED;
+    if (blocks * 256 > kMostThreads) return RNNT_ERR_UNSUPPORTED;
     auto run = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, static_cast<hipStream_t>(stream), x, (long long)rows, (long long)cols,
                            (long long)x_stride, static_cast<unsigned char *>(codes_out), static_cast<unsigned char *>(scales_out), values_out, ct, st);
@@ -681,7 +668,7 @@ int rnnt_mx4_product(const void *a, const void *a_scales, int32_t a_type, int64_
     if (plan == kDirect) {
         const int nt = direct_groups(M, N, 4) >= kDirectGroups ? 4 : 2;
         const int64_t blocks = direct_groups(M, N, nt);
-        if (blocks > kMost) return RNNT_ERR_UNSUPPORTED;
+        if (blocks > kMostThreads / 512) return RNNT_ERR_UNSUPPORTED;
         auto run = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(waves * 64), 0, on, args); };
         auto with = [&](auto t) {
             if (nt == 4) run(mx4_product_kernel<t(), 4, 4>, 4);
@@ -706,7 +693,7 @@ int rnnt_mx4_product(const void *a, const void *a_scales, int32_t a_type, int64_
         typedef decltype(shape) S;
         const auto kernel = mx4_tile_kernel<S, decltype(y)::value>;
         const int64_t mb = tiles(M, S::BM), nb = tiles(N, S::BN);
-        if (mb * nb > kMost / 8) return RNNT_ERR_UNSUPPORTED;
+        if (mb * nb > kMostThreads / 256) return RNNT_ERR_UNSUPPORTED;
         MX4_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS));
         const int64_t groups = S::CHAIN ? std::min<int64_t>(mb * nb, kComputeUnits * S::GROUPS) : mb * nb;
         hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), S::LDS, on, args, (int)mb, (int)nb);

@@ -33,7 +33,7 @@ def test_quantize(lib):
     assert f(x=None) == NULL and f(codes=None) == NULL and f(scales=None) == NULL
     assert f(type=3) == SHAPE and f(type=-1) == SHAPE and f(rows=-1) == SHAPE and f(cols=-1) == SHAPE and f(stride=63) == SHAPE
     assert f(x=P + 2) == SHAPE and f(x=P + 1, type=1) == SHAPE and f(codes=P + 8) == SHAPE and f(scales=P + 4) == SHAPE and f(values=P + 1) == SHAPE
-    assert f(rows=2 ** 31) == UNSUPPORTED
+    assert f(rows=2 ** 31) == UNSUPPORTED and f(rows=2 ** 31 - 1) == UNSUPPORTED and f(rows=2 ** 24, cols=2 ** 24, stride=2 ** 24) == UNSUPPORTED
 
 
 def test_product(lib):
@@ -46,6 +46,7 @@ def test_product(lib):
     assert f(a=P + 8) == SHAPE and f(a_scales=P + 4) == SHAPE and f(w=P + 4) == SHAPE and f(ws=P + 8) == SHAPE and f(bias=P + 2) == SHAPE
     assert f(y=P + 2) == SHAPE and f(y=P + 1, y_type=1) == SHAPE and f(a=P + 2, a_type=0, a_stride=128) == SHAPE
     assert f(M=2 ** 31) == UNSUPPORTED and f(K=2 ** 31) == UNSUPPORTED
+    assert f(M=2 ** 28, N=2 ** 20, y_stride=2 ** 20, K=0) == UNSUPPORTED and f(M=2 ** 31 - 1, N=2 ** 20, y_stride=2 ** 20) == UNSUPPORTED
     need = ctypes.c_int64(-1)
     g = lambda *k: (lib.rnnt_mx4_product_workspace(*k, ctypes.byref(need)), need.value)  # noqa: E731
     assert g(3, 8192, 8192, 8192) == (OK, 0) and g(0, 0, 5, 5) == (OK, 0) and g(0, 8, 5, 0) == (OK, 0)
@@ -68,7 +69,7 @@ def test_select(lib):
         assert f(**{k: P + 1}) == SHAPE
     assert f(type=3) == SHAPE and f(batch=-1) == SHAPE and f(beam=-1) == SHAPE and f(B=-1) == SHAPE and f(beams=0) == SHAPE and f(beams=65) == SHAPE
     assert f(V=0) == SHAPE and f(n=0) == SHAPE and f(n=65) == SHAPE and f(fin=P, end=1000) == SHAPE and f(fin=P, end=-1) == SHAPE and f(space_bytes=-1) == SHAPE
-    assert f(V=2 ** 30) == UNSUPPORTED
+    assert f(V=2 ** 30) == UNSUPPORTED and f(B=2 ** 31 - 1) == UNSUPPORTED and f(B=2 ** 24, n=40) == UNSUPPORTED
     need = ctypes.c_int64(-1)
     g = lambda *k: (lib.rnnt_beam_select_workspace(*k, ctypes.byref(need)), need.value)  # noqa: E731
     assert g(2, 65, 10, 1)[0] == SHAPE and g(2, 1, 10, 0)[0] == SHAPE and g(2, 64, 2 ** 26, 1)[0] == UNSUPPORTED and g(0, 1, 1, 1) == (OK, 0)
@@ -103,4 +104,4 @@ def test_reorder(lib):
     assert f(dst=P, src_batch=0, dst_batch=0) == SHAPE and f(dst=P, src_outer=0, dst_outer=0) == SHAPE
     assert f(B=0, dst_batch=0) == OK and f(outer=0, dst_outer=0) == OK
     assert f(dst=P, k_out=3) == SHAPE and f(dst=P, dst_batch=512) == SHAPE       # within itself: the same strides and beams
-    assert f(outer=2 ** 31) == UNSUPPORTED
+    assert f(outer=2 ** 31) == UNSUPPORTED and f(outer=2 ** 24) == UNSUPPORTED
