@@ -549,6 +549,16 @@ def _on_device(first, *others):
     return first.device
 
 
+def _workspace(given, need: int, device):
+    """A workspace of at least `need` bytes and its size: the given one, or a new one."""
+    import torch
+    if given is None:
+        return (torch.empty(need, dtype=torch.uint8, device=device), need) if need else (None, 0)
+    if given.dtype != torch.uint8 or not given.is_contiguous():
+        raise ValueError("workspace: a contiguous uint8 tensor is wanted")
+    return given, given.numel()
+
+
 def _rows_of(t, what: str):
     """The row stride of a matrix whose rows are contiguous."""
     if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
@@ -604,13 +614,10 @@ class Mx4Matrix:
         elif tuple(out.shape) != (M, self.rows) or (dtype is not None and out.dtype != dtype):
             raise ValueError(f"out: a {dtype or 'float'} matrix {(M, self.rows)} is wanted")
         out_stride, out_type = _rows_of(out, "out"), _type_of(out)
-        need = rnnt_mx4_product_workspace(a_type, M, self.rows, self.cols)
-        if workspace is None and need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        workspace, space = _workspace(workspace, rnnt_mx4_product_workspace(a_type, M, self.rows, self.cols), device)
         with torch.cuda.device(device):
             rnnt_mx4_product(codes, scales, a_type, stride, self.codes, self.scales, bias, out, out_type, out_stride,
-                             M, self.rows, self.cols, workspace, 0 if workspace is None else workspace.numel(),
-                             torch.cuda.current_stream().cuda_stream)
+                             M, self.rows, self.cols, workspace, space, torch.cuda.current_stream().cuda_stream)
         return out
 
 
@@ -634,15 +641,13 @@ def beam_select(logits, scores, n_out: Optional[int] = None, finished=None, end_
                                  or not finished.is_contiguous()):
         raise ValueError("finished: a contiguous uint8 or bool tensor [B, beams] is wanted")
     device = _on_device(logits, scores, finished, workspace)
-    need = rnnt_beam_select_workspace(B, beams, V, n_out)
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    workspace, space = _workspace(workspace, rnnt_beam_select_workspace(B, beams, V, n_out), device)
     best = torch.empty((B, n_out), dtype=torch.float32, device=device)
     tokens, parents = torch.empty((2, B, n_out), dtype=torch.int32, device=device)
     with torch.cuda.device(device):
         rnnt_beam_select(logits, _type_of(logits), logits.stride(0), logits.stride(1), scores, finished, B, beams, V,
-                         n_out, int(end_token), best, tokens, parents, workspace,
-                         0 if workspace is None else workspace.numel(), torch.cuda.current_stream().cuda_stream)
+                         n_out, int(end_token), best, tokens, parents, workspace, space,
+                         torch.cuda.current_stream().cuda_stream)
     return best, tokens, parents
 
 

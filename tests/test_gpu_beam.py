@@ -260,7 +260,9 @@ def test_refusals_of_tensors_that_do_not_fit(pkg):  # noqa: F811
     import torch
     x, s = torch.randn((2, 3, 10), device="cuda"), torch.zeros((2, 3), device="cuda")
     for bad in (lambda: pkg.beam_select(x[0], s), lambda: pkg.beam_select(x, s[:1]), lambda: pkg.beam_select(x, s.double()),
-                lambda: pkg.beam_select(x.transpose(1, 2), s), lambda: pkg.beam_select(x, s.cpu()), lambda: pkg.beam_select(x, s, finished=s)):
+                lambda: pkg.beam_select(x.transpose(1, 2), s), lambda: pkg.beam_select(x, s.cpu()), lambda: pkg.beam_select(x, s, finished=s),
+                lambda: pkg.beam_select(x, s, workspace=torch.empty((1,), dtype=torch.uint8, device="cuda").expand(1 << 20)),
+                lambda: pkg.beam_select(x, s, workspace=torch.empty((64,), device="cuda"))):
         with pytest.raises(ValueError):
             bad()
     with pytest.raises(TypeError):

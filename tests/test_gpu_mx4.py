@@ -223,6 +223,69 @@ def test_products_on_another_stream_and_from_a_graph(pkg):  # noqa: F811
             assert torch.equal(y, want[i])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(3, 18, 97), (20, 40, 256), (2100, 640, 320), (1500, 1301, 450)])
+def test_addresses_that_are_multiples_of_an_element_only(pkg, M, N, K, dtype):  # noqa: F811
+    """Operands and results that begin one element behind an aligned address, with rows of odd and of even distances."""
+    import torch
+    g = torch.Generator().manual_seed(M + N + K)
+    t = _torch_type(dtype)
+    w = torch.randn((N, K), generator=g)
+    for pad in (1, 2):
+        a = torch.randn((M, K + pad), generator=g).to(t)
+        part = a.cuda()[:, 1:K + 1] if pad > 1 else a.cuda().flatten()[1:].as_strided((M, K), (K + 1, 1))
+        x = part.cpu().clone()
+        code, scale, val = quantize(x.double().numpy())
+        m = pkg.Mx4Matrix(M, K, "cuda").quantize(part)
+        wc, ws = layout(code, scale)
+        assert np.array_equal(m.codes.cpu().numpy(), wc) and np.array_equal(m.scales.cpu().numpy(), ws)
+        out = torch.full((M, N + pad + 1), 99.0, dtype=t, device="cuda")
+        got = pkg.mx4_quantize(w.cuda()).product(part, out=out[:, 1:N + 1])
+        _check_product(got.double().cpu().numpy(), val, quantize(w.double().numpy())[2], None, dtype, K)
+        assert (out[:, 0] == 99).all() and (out[:, N + 1:] == 99).all()
+
+
+def test_rows_beyond_32_bit_offsets(pkg):  # noqa: F811
+    """Rows 2^30 elements apart, of the operand and of the result: the last ones lie beyond 2^32 bytes and 2^31 elements."""
+    import torch
+    M, N, K, far = 4, 37, 300, 1 << 30
+    g = torch.Generator().manual_seed(12)
+    a, w = torch.randn((M, K), generator=g).bfloat16(), torch.randn((N, K), generator=g)
+    store = torch.empty((M - 1) * far + 1024, dtype=torch.bfloat16, device="cuda")
+    x, y = store.as_strided((M, K), (far, 1)), store.as_strided((M, N), (far, 1), 512)
+    x.copy_(a)
+    code, scale, val = quantize(a.double().numpy())
+    assert np.array_equal(pkg.mx4_quantize(x).codes.cpu().numpy(), layout(code, scale)[0])
+    pkg.mx4_quantize(w.cuda()).product(x, out=y)
+    _check_product(y.double().cpu().numpy(), val, quantize(w.double().numpy())[2], None, "bf16", K)
+    assert torch.equal(x.cpu(), a)
+
+
+def test_a_large_product_from_a_graph_beside_eager_ones(pkg):  # noqa: F811
+    """Large tiles, replayed while another stream computes products of its own with a workspace of its own."""
+    import torch
+    g = torch.Generator().manual_seed(13)
+    M, N, K = 4200, 4100, 390
+    w = pkg.mx4_quantize(torch.randn((N, K), generator=g).cuda())
+    xs = [torch.randn((M, K), generator=g).cuda() for _ in range(2)]
+    want = [w.product(x) for x in xs]
+    x, y, z = xs[0].clone(), torch.empty_like(want[0]), torch.empty_like(want[0])
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        w.product(x, out=y)
+    for i in (1, 0, 1):
+        x.copy_(xs[i])
+        y.fill_(0), z.fill_(0)
+        torch.cuda.synchronize()
+        graph.replay()
+        with torch.cuda.stream(side):
+            w.product(xs[1 - i], out=z)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[i]) and torch.equal(z, want[1 - i])
+
+
 def test_refusals_of_tensors_that_do_not_fit(pkg):  # noqa: F811
     import torch
     w = pkg.mx4_quantize(torch.randn((5, 64), device="cuda"))
@@ -238,5 +301,8 @@ def test_refusals_of_tensors_that_do_not_fit(pkg):  # noqa: F811
         w.product(torch.randn((3, 64), device="cuda"), bias=torch.zeros(4, device="cuda"))
     with pytest.raises(ValueError):
         w.product(torch.randn((3, 64), device="cuda"), out=torch.zeros((3, 6), device="cuda"))
+    for space in (torch.empty((1,), dtype=torch.uint8, device="cuda").expand(1 << 20), torch.empty((64,), device="cuda")):
+        with pytest.raises(ValueError):
+            w.product(torch.randn((3, 64), device="cuda"), workspace=space)
     with pytest.raises(ValueError):
         w.quantize(torch.randn((5, 65), device="cuda"))
