@@ -101,6 +101,39 @@ def test_short_rows(pkg, B, beams, V, n, dtype):  # noqa: F811
     _check(pkg, x, far, n)
 
 
+@pytest.mark.parametrize("B,beams,V,n", [(3, 5, 300, 5), (2, 40, 1025, 40), (2, 3, 30000, 3)])
+def test_selection_and_reordering_on_another_stream_and_from_a_graph(pkg, B, beams, V, n):  # noqa: F811
+    """Short rows, lists and two launches, replayed beside eager calls on another stream."""
+    import torch
+    g = torch.Generator().manual_seed(V)
+    xs = [torch.randn((B, beams, V), generator=g).cuda() for _ in range(2)]
+    scores, state = -torch.rand((B, beams), generator=g).cuda(), torch.randn((B, beams, 77), generator=g).cuda()
+
+    def step(x, dst):
+        best = pkg.beam_select(x, scores, n)
+        pkg.beam_reorder([(state, dst)], best[2])
+        return (*best, dst)
+    want = [step(x, torch.empty_like(state)) for x in xs]
+    for x, w in zip(xs, want):
+        check_selection(tuple(t.cpu().numpy() for t in w[:3]), totals(x.double().cpu().numpy(), scores.cpu().numpy()), x.double().cpu().numpy(), n)
+        assert np.array_equal(w[3].cpu().numpy(), _reorder(state.cpu().numpy(), w[2].cpu().numpy(), beams))
+    side, x, dst = torch.cuda.Stream(), xs[0].clone(), torch.empty_like(state)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(x, dst)
+    for i in (1, 0, 1, 1):
+        x.copy_(xs[i])
+        for t in out:
+            t.fill_(5)
+        torch.cuda.synchronize()
+        graph.replay()
+        with torch.cuda.stream(side):
+            other = step(xs[1 - i], torch.empty_like(state))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want[i])) and all(torch.equal(a, b) for a, b in zip(other, want[1 - i]))
+
+
 def test_zeros_of_either_sign_tie(pkg):  # noqa: F811
     import torch
     x = torch.full((1, 1, 100), -1.0)
