@@ -141,10 +141,14 @@ template <class F> __device__ __forceinline__ F wave_max(F v)
     v = larger(v, from_lane<1>(v)); v = larger(v, from_lane<2>(v)); v = larger(v, from_lane<4>(v));
     v = larger(v, from_lane<8>(v)); v = larger(v, from_lane<16>(v)); return larger(v, from_lane<32>(v));
 }
+// (The first lane's sum for all of them: where v is a product that the compiler fuses with the first addition, the lanes' differ in their last
+// bit, and equal logits would no longer have equal scores.)
 __device__ __forceinline__ double wave_sum(double v)
 {
     v += from_lane<1>(v); v += from_lane<2>(v); v += from_lane<4>(v);
-    v += from_lane<8>(v); v += from_lane<16>(v); return v + from_lane<32>(v);
+    v += from_lane<8>(v); v += from_lane<16>(v); v += from_lane<32>(v);
+    const u64 u = __builtin_bit_cast(u64, v);
+    return __builtin_bit_cast(double, (u64)(unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)u));
 }
 
 constexpr float kLog2E = 1.44269504f, kLowest = -3.402823466e38f;

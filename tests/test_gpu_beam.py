@@ -101,6 +101,19 @@ def test_short_rows(pkg, B, beams, V, n, dtype):  # noqa: F811
     _check(pkg, x, far, n)
 
 
+@pytest.mark.parametrize("B,beams,V,n", [(256, 16, 1025, 16), (256, 16, 1500, 16), (64, 16, 4097, 16), (16, 16, 9000, 16), (16, 8, 40000, 40), (256, 4, 1500, 40)])
+def test_equal_logits_of_a_row_stay_in_order(pkg, B, beams, V, n):  # noqa: F811
+    """Logits of few bits beside scores of many: what a row has twice has one score, and the lower token comes first."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = (torch.randn((B, beams, V), generator=g, device="cuda") * 3).bfloat16()
+    scores = torch.rand((B, beams), generator=g, device="cuda") * -20
+    best, tokens, parents = pkg.beam_select(x, scores, n)
+    at = x.gather(1, parents.long()[..., None].expand(-1, -1, V)).gather(2, tokens.long()[..., None])[..., 0]
+    tie = (parents[:, 1:] == parents[:, :-1]) & (at[:, 1:] == at[:, :-1])
+    assert int(tie.sum()) >= 3 and (best[:, 1:] == best[:, :-1])[tie].all() and (tokens[:, 1:] > tokens[:, :-1])[tie].all()
+
+
 @pytest.mark.parametrize("B,beams,V,n", [(3, 5, 300, 5), (2, 40, 1025, 40), (2, 3, 30000, 3)])
 def test_selection_and_reordering_on_another_stream_and_from_a_graph(pkg, B, beams, V, n):  # noqa: F811
     """Short rows, lists and two launches, replayed beside eager calls on another stream."""
