@@ -152,6 +152,9 @@ __device__ __forceinline__ double wave_sum(double v)
 }
 
 constexpr float kLog2E = 1.44269504f, kLowest = -3.402823466e38f;
+// Differences of x log2(e) to a rounded shift are off by half a step of the shift, a power of two at 2^24 and beyond all floats at 2^31: where the largest
+// logit of all is as far out as kFar, differences of logits are taken, and a lane with lower ones only has the shift kLeast and adds nothing.
+constexpr float kFar = 0x1p23f, kLeast = -0x1p24f;
 
 // One pass over a piece of a row by a wave: the running maximum and sum of a softmax, a lane's own, and the best n of its
 // logits.  A tile is 16 logits a lane (and 64 more where the row ends with them: vocabularies are a power of two and a blank).
@@ -243,7 +246,7 @@ template <class T, int WIDTH, bool LONG> struct Scan {
 #pragma unroll
             for (int i = 1; i < ALL; ++i) m = fmaxf(m, f[i]);
             top = fmaxf(top, m);
-            const float now = fmaxf(top * kLog2E, kLowest);
+            const float now = fmaxf(top * kLog2E, kLeast);
             float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < ALL; ++i) part[i % 4] += __builtin_amdgcn_exp2f(__builtin_fmaf(f[i], kLog2E, -now));
@@ -288,13 +291,12 @@ template <class T, int WIDTH, bool LONG> struct Scan {
             base += size;
         }
         top = wave_max(top);
-        if (!(fabsf(top) < 2.3e38f)) { far(from, to); return; }
+        if (!(fabsf(top) < kFar)) { far(from, to); return; }
         const float all = wave_max(shift);
         sum = wave_sum(sum * (double)__builtin_amdgcn_exp2f(shift - all));
         ref = (double)all / (double)kLog2E;
     }
-    // A row whose largest logit has a product with log2(e) beyond the largest float (a mask of the type's lowest value, or of -inf, in
-    // all of it; an infinity): the terms are made of differences to the largest logit.
+    // A row whose largest logit is far out (a mask in all of it; an infinity): the terms are made of differences to it.
     __device__ __forceinline__ void far(int from, int to)
     {
         sum = 0;

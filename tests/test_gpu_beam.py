@@ -147,6 +147,24 @@ def test_selection_and_reordering_on_another_stream_and_from_a_graph(pkg, B, bea
         assert all(torch.equal(a, b) for a, b in zip(out, want[i])) and all(torch.equal(a, b) for a, b in zip(other, want[1 - i]))
 
 
+@pytest.mark.parametrize("V,n", [(40, 20), (1025, 4), (1025, 20), (3000, 9), (9000, 20), (30000, 5), (30000, 40)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_masks_of_finite_values(pkg, V, n, dtype):  # noqa: F811
+    """Logits of the order of one beside masks of any size, and rows that are all mask, or all large."""
+    import torch
+    g = torch.Generator().manual_seed(V + n)
+    most = float(torch.finfo(_torch_type(dtype)).max)
+    values = [v for v in (1e4, 6e4, 1e7, 1e9, 1e10, 1e20, 1e30, 1e38) if v < most]
+    x = torch.randn((2 * len(values), 3, V), generator=g)
+    few = torch.rand((3, V), generator=g) < 0.98
+    for i, v in enumerate(values):
+        x[2 * i, 0] = torch.where(few[0], -v, x[2 * i, 0])
+        x[2 * i, 1, : V - 1], x[2 * i, 2] = -v, -v
+        x[2 * i + 1, 0, ::3], x[2 * i + 1, 1], x[2 * i + 1, 2, V // 2] = v, v, v
+    scores = -torch.rand((2 * len(values), 3), generator=g)
+    _check(pkg, x.to(_torch_type(dtype)), scores, n)
+
+
 def test_zeros_of_either_sign_tie(pkg):  # noqa: F811
     import torch
     x = torch.full((1, 1, 100), -1.0)
