@@ -18,6 +18,8 @@ constexpr int kBuffer = 128;            // candidates of a wave that wait to be 
 constexpr int kJoinWaves = 16;          // waves of a work-group that joins lists, at most
 
 typedef unsigned long long u64;
+typedef unsigned v2u __attribute__((ext_vector_type(2)));
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
 struct SelectArgs {
     const void *logits;
@@ -526,32 +528,147 @@ beam_short_kernel(const SelectArgs a)
     }
 }
 
-// Few utterances with long rows: pieces over the whole device, joined by a second launch.  A work-group's waves have four pieces
-// of a row and join them, two by two.
+// Long rows: pieces over the whole device, joined by a second launch.  A work-group's waves have four pieces
+// of a row and join their lists, two by two.
 constexpr int kScanWaves = 4;
+struct ScanLds { u64 buffers[kScanWaves][kBuffer]; double sums[kScanWaves], refs[kScanWaves]; };
+struct Piece { unsigned hyp, b; int from, to; };
+__device__ __forceinline__ Piece piece_of(const SelectArgs &a, int wave)
+{
+    const unsigned hyp = blockIdx.x / a.pieces;
+    const long long piece = (long long)(blockIdx.x - hyp * a.pieces) * kScanWaves + wave;
+    return {hyp, hyp / a.beams, (int)min(piece * a.piece_tiles * kTile, (long long)a.V), (int)min((piece + 1) * a.piece_tiles * kTile, (long long)a.V)};
+}
+__device__ __forceinline__ void store_piece(const SelectArgs &a, const ScanLds &lds, int lane, u64 key)
+{
+    if (lane < a.n_out) a.lists[(long long)blockIdx.x * a.n_out + lane] = key;
+    if (lane < kScanWaves) { a.sums[(long long)blockIdx.x * kScanWaves + lane] = lds.sums[lane]; a.refs[(long long)blockIdx.x * kScanWaves + lane] = lds.refs[lane]; }
+}
+template <int TYPE, int WIDTH>
+__device__ __forceinline__ void scan_pieces(const SelectArgs &a, ScanLds &lds)
+{
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const Piece p = piece_of(a, wave);
+    auto s = scan_of<typename Logit<TYPE>::T, WIDTH, true>(a, (int)p.b, (int)(p.hyp - p.b * a.beams), lds.buffers[wave]);
+    s.begin(p.from, p.to);
+    if ((a.finished && a.finished[p.hyp]) || !(a.scores[p.hyp] > -INFINITY)) return;       // (the whole work-group)
+    s.run(p.from, p.to);
+    if (lane == 0) { lds.sums[wave] = s.sum; lds.refs[wave] = s.ref; }
+    for (int half = kScanWaves / 2; half > 0; half /= 2) {
+        if (wave >= half && wave < 2 * half && lane < WIDTH) lds.buffers[wave][lane] = s.list.key;
+        __syncthreads();
+        if (wave < half) join<WIDTH>(s.list, InRow{lds.buffers[wave + half][WIDTH - 1 - lane % WIDTH]});
+    }
+    if (wave == 0) store_piece(a, lds, lane, s.list.key);
+}
 template <int TYPE, int WIDTH>
 __global__ void __launch_bounds__(kScanWaves * 64)
 beam_scan_kernel(const SelectArgs a)
 {
-    __shared__ u64 buffers[kScanWaves][kBuffer];
-    __shared__ double sums[kScanWaves], refs[kScanWaves];
+    __shared__ ScanLds lds;
+    scan_pieces<TYPE, WIDTH>(a, lds);
+}
+
+// The same for few winners and pieces that a wave holds as a whole, kHeld loads a lane.  The lanes' largest logits in the four pieces are 64
+// different ones; the n-th of them bounds the n-th best from below, and what is not below it, for n = 8 about nine logits of four pieces, is the
+// list.  Where ties make more than 64 of them, the work-group does its pieces the other way.  Bound by memory, and by the exponentials behind it: 67 MB
+// of f16 logits (64 x 8 rows of 65535) 17.5 us (lists: 24), 14 without the sums and the list.
+constexpr int kHeld = 16, kHeldWinners = 16;
+template <class T> constexpr int held_size() { return kHeld * 64 * 16 / (int)sizeof(T); }
+template <int TYPE>
+__global__ void __launch_bounds__(kScanWaves * 64, 4)
+beam_held_kernel(const SelectArgs a)
+{
+    typedef typename Logit<TYPE>::T T;
+    constexpr int PER = 16 / (int)sizeof(T);
+    struct __attribute__((packed, aligned(sizeof(T)))) At { T e[PER]; };
+    __shared__ ScanLds lds;
+    __shared__ u64 found[64];
+    __shared__ unsigned group[64];
+    __shared__ int found_count;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const unsigned hyp = blockIdx.x / a.pieces, b = hyp / a.beams;
-    const long long piece = (long long)(blockIdx.x - hyp * a.pieces) * kScanWaves + wave;
-    const int from = (int)min(piece * a.piece_tiles * kTile, (long long)a.V), to = (int)min((piece + 1) * a.piece_tiles * kTile, (long long)a.V);
-    auto s = scan_of<typename Logit<TYPE>::T, WIDTH, true>(a, (int)b, (int)(hyp - b * a.beams), buffers[wave]);
-    s.begin(from, to);
-    if ((a.finished && a.finished[hyp]) || !(a.scores[hyp] > -INFINITY)) return;       // (the whole work-group)
-    s.run(from, to);
-    if (lane == 0) { sums[wave] = s.sum; refs[wave] = s.ref; }
-    for (int half = kScanWaves / 2; half > 0; half /= 2) {
-        if (wave >= half && wave < 2 * half && lane < WIDTH) buffers[wave][lane] = s.list.key;
-        __syncthreads();
-        if (wave < half) join<WIDTH>(s.list, InRow{buffers[wave + half][WIDTH - 1 - lane % WIDTH]});
+    const Piece p = piece_of(a, wave);
+    const int rest = p.to - p.from;
+    const T *row = static_cast<const T *>(a.logits) + p.b * a.batch_stride + (p.hyp - p.b * a.beams) * a.beam_stride + p.from;
+    // A load that would go on behind the piece's end is the last one before it (a row has PER logits or more); `twice`
+    // of its logits are another load's, or another wave's.
+    auto off = [&](int q) { return min((q * 64 + lane) * PER, rest - PER); };
+    At held[kHeld];
+#pragma unroll
+    for (int q = 0; q < kHeld; ++q) held[q] = *reinterpret_cast<const At *>(row + off(q));
+    if ((a.finished && a.finished[p.hyp]) || !(a.scores[p.hyp] > -INFINITY)) return;       // (the whole work-group)
+    if (wave == 0) { group[lane] = 0; if (lane == 0) found_count = 0; }
+    // The sum is of differences to the largest logit of the first load, so that it is made while others are on their way; where that
+    // turns out to be far from the largest one of all, it is made again.
+    float most[kHeld], m = -INFINITY, now = 0.f, first = kLowest, part[2] = {0.f, 0.f};
+    double sum = 0, ref;
+#pragma unroll
+    for (int q = 0; q < kHeld; ++q) {
+        most[q] = -INFINITY;
+        if (q * 64 * PER >= rest) continue;
+        if ((q + 1) * 64 * PER > rest) {
+            const int twice = (q * 64 + lane) * PER - off(q);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) if (e < twice) held[q].e[e] = (T)-INFINITY;
+        }
+#pragma unroll
+        for (int e = 0; e < PER; ++e) most[q] = fmaxf(most[q], (float)held[q].e[e]);
+        m = fmaxf(m, most[q]);
+        if (q == 0) { first = wave_max(fmaxf(m, kLowest)); now = first * kLog2E; }
+#pragma unroll
+        for (int e = 0; e < PER; ++e) part[e % 2] += __builtin_amdgcn_exp2f(__builtin_fmaf((float)held[q].e[e], kLog2E, -now));
+        if ((q + 1) * PER % 16 == 0 || (q + 1) * 64 * PER >= rest) { sum += (double)(part[0] + part[1]); part[0] = part[1] = 0.f; }
+    }
+    const float top = wave_max(fmaxf(m, kLowest));
+    if (!(top - first < 60.f) || !(fabsf(first) < kFar)) {
+        sum = 0;
+#pragma unroll 1
+        for (int j = lane; j < rest; j += 64) sum += (double)__builtin_amdgcn_exp2f(((float)row[j] - top) * kLog2E);
+        ref = (double)top;
+    } else ref = (double)now / (double)kLog2E;
+    sum = wave_sum(sum);
+    if (lane == 0) { lds.sums[wave] = sum; lds.refs[wave] = ref; }
+    __syncthreads();                                       // (the cleared LDS)
+    if (m > -INFINITY) atomicMax(&group[lane], (unsigned)(row_key(m, 0) >> 32));
+    __syncthreads();
+    const unsigned best = group[lane];
+    unsigned nth = 0;                                      // (its highest 20 bits: from a little lower on)
+#pragma unroll
+    for (int bit = 31; bit >= 12; --bit) if (__popcll(__ballot(best >= (nth | 1u << bit))) >= a.n_out) nth |= 1u << bit;
+    const float low = fmaxf(key_logit((u64)nth << 32), kLowest);
+    // (widened anew: kept, they would take twice the registers)
+#pragma unroll
+    for (int q = 0; q < kHeld; ++q) {
+        v4u raw = __builtin_bit_cast(v4u, held[q]);
+        asm volatile("" : "+v"(raw));
+        held[q] = __builtin_bit_cast(At, raw);
+    }
+#pragma unroll
+    for (int q = 0; q < kHeld; ++q) {
+        if (__ballot(most[q] >= low) == 0ull) continue;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            const float x = (float)held[q].e[e];
+            if (x >= low) {
+                const int at = atomicAdd(&found_count, 1);
+                if (at < 64) found[at] = row_key(x, p.from + off(q) + e);
+            }
+        }
+    }
+    __syncthreads();
+    const int count = found_count;
+    if (count > 64) {                                      // (the whole work-group)
+        scan_pieces<TYPE, 16>(a, lds);
+        return;
     }
     if (wave != 0) return;
-    if (lane < a.n_out) a.lists[(long long)blockIdx.x * a.n_out + lane] = s.list.key;
-    if (lane < kScanWaves) { a.sums[(long long)blockIdx.x * kScanWaves + lane] = sums[lane]; a.refs[(long long)blockIdx.x * kScanWaves + lane] = refs[lane]; }
+    InRow v{lane < count ? found[lane] : 0};
+    if (count <= 16) sort_lanes<16>(v);
+    else {
+        sort_lanes<64>(v);
+        v = v.template lane<16>().template lane<32>();     // the best 16, worst first, to lanes 0 .. 15
+    }
+    store_piece(a, lds, lane, reverse<16>(v).key);
 }
 template <int WIDTH>
 __global__ void __launch_bounds__(kJoinWaves * 64)
@@ -609,8 +726,6 @@ struct ReorderArgs {
     int n, B, beams_in, beams_out;
 };
 
-typedef unsigned v2u __attribute__((ext_vector_type(2)));
-typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
 // Memory bound.  Eight loads of a thread are on their way together, whatever rows they are of.  STREAM: the stores are marked as not
 // to be kept in the L2s, for calls that write more than those hold (kStreamBytes).  128 utterances of 16 beams, 67 MB of
@@ -728,25 +843,32 @@ constexpr int64_t kMostThreads = 0xffffffff;                                // o
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 // How a selection is cut up.  One launch, a work-group an utterance and a wave a row, where that leaves a wave no more than
-// kOneLaunchTiles tiles, or where the rows fill the device: the second launch costs what a wave takes for several tiles.  Else
-// pieces of two tiles or more, towards sixteen waves on every compute unit.
-constexpr int kOneLaunchTiles = 8, kWavesWanted = 4096;
+// kOneLaunchTiles tiles: the second launch costs what a wave takes for several tiles.  Else pieces of two tiles or more, towards sixteen waves on
+// every compute unit.  Pieces that waves hold are read at the rate of memory however many there are: of few rows they pay from kFewTiles
+// on, and no number of rows is too large for them; lists are made in one launch where there are kWavesWanted rows.  us, one launch and two: 64 x 16
+// rows of 8000 bf16 logits for 16 winners 28.1 and 14.1, 64 x 4 of 5000 fp32 for 4 11.9 and 8.7, but 128 x 4 of 2049 fp32 for 4 8.4 and 9.0,
+// 128 x 16 of 4097 bf16 for 16 20.2 and 22.5, 1024 x 4 of 4097 for 4 17.7 and 30; 512 x 4 of 65537 for 4 69 (lists) and 54.
+constexpr int kOneLaunchTiles = 8, kFewTiles = 4, kFewRows = 2048, kWavesWanted = 4096, kMostPieces = 64 / kScanWaves;
 
 struct SelectPlan {
-    bool two = false, is_short = false;
+    bool two = false, is_short = false, held = false;
     int pieces = 1, piece_tiles = 1, waves = 1;
     size_t lds = 0;
     int64_t bytes = 0;
-    SelectPlan(int64_t B, int beams, int V, int n)
+    SelectPlan(int type, int64_t B, int beams, int V, int n)
     {
         const int row = (V - 1) / kTile + 1;
         while (waves < kJoinWaves && waves < beams) waves *= 2;
         is_short = V <= kShortRow && beams >= kShortRows && beams <= kJoinWaves && n <= kShortWinners;
         lds = std::max(join_lds(waves, beams, n), is_short ? sizeof(ShortLds) : 0);
-        if ((beams + waves - 1) / waves * row <= kOneLaunchTiles || B * beams >= kWavesWanted) return;
+        // (rows that waves hold as a whole: in no more pieces than the join takes)
+        const int most = (type == RNNT_TYPE_F32 ? held_size<float>() : held_size<__bf16>()) / kTile;
+        held = n <= kHeldWinners && V >= 8 && (row + most * kScanWaves - 1) / (most * kScanWaves) <= kMostPieces;
+        if ((beams + waves - 1) / waves * row <= (held && B * beams < kFewRows ? kFewTiles : kOneLaunchTiles) || (!held && B * beams >= kWavesWanted)) return;
         two = true;
-        const int64_t into = std::min<int64_t>(std::max<int64_t>(kWavesWanted / (B * beams * kScanWaves), 1), std::min(64 / kScanWaves, (row + 2 * kScanWaves - 1) / (2 * kScanWaves)));
+        const int64_t into = std::min<int64_t>(std::max<int64_t>(kWavesWanted / (B * beams * kScanWaves), 1), std::min(kMostPieces, (row + 2 * kScanWaves - 1) / (2 * kScanWaves)));
         piece_tiles = (int)((row + into * kScanWaves - 1) / (into * kScanWaves));
+        if (held) piece_tiles = std::min(piece_tiles, most);
         pieces = (row + piece_tiles * kScanWaves - 1) / (piece_tiles * kScanWaves);
         bytes = B * beams * pieces * (n * 8 + kScanWaves * 16);
     }
@@ -761,7 +883,8 @@ int rnnt_beam_select_workspace(int32_t B, int32_t beams, int32_t V, int32_t n_ou
     if (!bytes_out) return RNNT_ERR_NULL;
     if (B < 0 || beams < 1 || beams > kMaxBeams || V < 1 || n_out < 1 || n_out > kMaxBeams) return RNNT_ERR_SHAPE;
     if ((int64_t)beams * V > 0x7fffffff) return RNNT_ERR_UNSUPPORTED;
-    *bytes_out = B > 0 ? SelectPlan(B, beams, V, n_out).bytes : 0;
+    // (enough for logits of any type)
+    *bytes_out = B > 0 ? std::max(SelectPlan(RNNT_TYPE_F32, B, beams, V, n_out).bytes, SelectPlan(RNNT_TYPE_BF16, B, beams, V, n_out).bytes) : 0;
     return RNNT_OK;
 }
 
@@ -780,7 +903,7 @@ int rnnt_beam_select(const void *logits, int32_t type, int64_t batch_stride, int
     if (!aligned(logits, type == RNNT_TYPE_F32 ? 4 : 2) || !aligned(scores, 4) || !aligned(scores_out, 4) || !aligned(tokens_out, 4) ||
         !aligned(parents_out, 4)) return RNNT_ERR_SHAPE;
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return RNNT_ERR_SCRATCH;
-    const SelectPlan p(B, beams, V, n_out);
+    const SelectPlan p(type, B, beams, V, n_out);
     if ((int64_t)B * p.waves * 64 > kMostThreads) return RNNT_ERR_UNSUPPORTED;
     SelectArgs args{logits, scores, finished, scores_out, tokens_out, parents_out, batch_stride, beam_stride, B, beams, V, n_out, end_token,
                     p.pieces, p.piece_tiles, nullptr, nullptr, nullptr};
@@ -804,7 +927,11 @@ int rnnt_beam_select(const void *logits, int32_t type, int64_t batch_stride, int
     args.sums = reinterpret_cast<double *>(args.lists + n * n_out);
     args.refs = args.sums + n * kScanWaves;
     auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(kScanWaves * 64), 0, on, args); };
-    auto with = [&](auto t) { if (n_out <= 16) run(beam_scan_kernel<t(), 16>); else run(beam_scan_kernel<t(), 64>); };
+    auto with = [&](auto t) {
+        if (p.held) run(beam_held_kernel<t()>);
+        else if (n_out <= 16) run(beam_scan_kernel<t(), 16>);
+        else run(beam_scan_kernel<t(), 64>);
+    };
     if (type == RNNT_TYPE_F32) with(std::integral_constant<int, RNNT_TYPE_F32>());
     else if (type == RNNT_TYPE_BF16) with(std::integral_constant<int, RNNT_TYPE_BF16>());
     else with(std::integral_constant<int, RNNT_TYPE_F16>());

@@ -32,7 +32,8 @@ def _check(pkg, x, scores, n, finished=None, end=0):  # noqa: F811
 
 
 CASES = [(1, 1, 1, 1), (1, 1, 5, 5), (2, 3, 7, 9), (1, 4, 1025, 4), (3, 8, 1025, 8), (2, 16, 257, 16), (5, 5, 64, 3), (1, 64, 130, 64), (2, 33, 1000, 33),
-         (1, 2, 4096, 64), (2, 4, 8193, 10), (1, 1, 65535, 64), (3, 7, 20001, 12), (1, 64, 20000, 64), (130, 2, 100, 2), (1, 3, 3, 20)]
+         (1, 2, 4096, 64), (2, 4, 8193, 10), (1, 1, 65535, 64), (3, 7, 20001, 12), (1, 64, 20000, 64), (130, 2, 100, 2), (1, 3, 3, 20),
+         (1, 2, 8192, 5), (2, 1, 32769, 16), (3, 2, 65543, 4), (1, 1, 262145, 8), (1, 1, 524289, 3), (1050, 2, 9001, 2), (40, 30, 1030, 7)]
 
 
 @pytest.mark.parametrize("B,beams,V,n", CASES)
@@ -50,7 +51,7 @@ def test_selection(pkg, B, beams, V, n, dtype):  # noqa: F811
     _check(pkg, x.to(_torch_type(dtype)), scores, n, finished, end=V // 2)
 
 
-@pytest.mark.parametrize("V,n", [(50, 10), (1025, 64), (9000, 64), (40000, 17)])
+@pytest.mark.parametrize("V,n", [(50, 10), (1025, 64), (9000, 64), (40000, 17), (9000, 10), (40000, 16), (1500, 9)])
 def test_ties_go_to_the_lowest_place(pkg, V, n):  # noqa: F811
     """Few different values, equal rows and equal scores: the order is by value, then hypothesis, then token."""
     import torch
@@ -165,6 +166,25 @@ def test_masks_of_finite_values(pkg, V, n, dtype):  # noqa: F811
     _check(pkg, x.to(_torch_type(dtype)), scores, n)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_long_rows_whose_first_logits_say_nothing(pkg, dtype):  # noqa: F811
+    """The largest logits far from the first ones, the first ones masked or very large, and values at the type's ends."""
+    import torch
+    g = torch.Generator().manual_seed(5)
+    low, inf = float(torch.finfo(_torch_type(dtype)).min), float("inf")
+    x = torch.randn((8, 2, 40000), generator=g)
+    x[0, :, :600] = -inf
+    x[1, :, :600] = low
+    x[2, :, 20000:] += 200
+    x[3, :, :8192] = -inf                                 # all of a piece and more
+    x[4, :, 100:] = -inf
+    x[5] = low
+    x[6, :, :700] = -low
+    x[7, :, ::3] = -low / 2
+    scores = -torch.rand((8, 2), generator=g)
+    _check(pkg, x.to(_torch_type(dtype)), scores, 9)
+
+
 def test_zeros_of_either_sign_tie(pkg):  # noqa: F811
     import torch
     x = torch.full((1, 1, 100), -1.0)
@@ -173,11 +193,12 @@ def test_zeros_of_either_sign_tie(pkg):  # noqa: F811
     assert v[0].tolist() == [10, 20, 30, 0]
 
 
-@pytest.mark.parametrize("V", [40, 1025, 12000])
+@pytest.mark.parametrize("V", [40, 1025, 12000, 30000])
 def test_masks_infinities_and_nan(pkg, V):  # noqa: F811
     import torch
     inf, nan = float("inf"), float("nan")
     g = torch.Generator().manual_seed(V)
+    n = 16 if V == 30000 else 20
     x = torch.randn((7, 4, V), generator=g)
     scores = -torch.rand((7, 4), generator=g)
     x[0, :, 3:] = -inf                                    # three tokens of each hypothesis are left
@@ -194,11 +215,11 @@ def test_masks_infinities_and_nan(pkg, V):  # noqa: F811
         if t != "f32":
             y[5] = torch.finfo(y.dtype).min
             y[5, 2, 7] = 0
-        got = _check(pkg, y, scores, 20)
+        got = _check(pkg, y, scores, n)
         assert (got[1][3] == -1).all() and (got[1][4] == -1).all()
     done = torch.zeros((7, 4), dtype=torch.bool)
     done[2], done[3, 1], done[4, 0] = True, True, True     # a finished hypothesis' logits do not matter; one that does not exist stays away
-    _check(pkg, x, scores, 20, done, end=V - 1)
+    _check(pkg, x, scores, n, done, end=V - 1)
 
 
 def test_values_far_apart(pkg):  # noqa: F811
