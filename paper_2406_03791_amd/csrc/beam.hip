@@ -389,13 +389,13 @@ beam_select_kernel(const SelectArgs a)
     select_rows<TYPE, WIDTH>(a, lds);
 }
 
-// Short rows (a tile and a last lane each), a wave a row, few winners: no lists.  The lanes' largest candidates over all rows are 64 different
-// ones; the n-th of those bounds the n-th best of the utterance from below, and what is not below the bound, for n = 16 about
-// 18 candidates of independent logits, is put together in LDS and ranked by counting.  Where ties make more than
+// Short rows (a tile and a last lane each), a wave for one or two of them, few winners: no lists.  The lanes' largest candidates over all rows are 64
+// different ones; the n-th of those bounds the n-th best of the utterance from below, and what is not below the bound, for n = 16 about
+// 18 candidates of independent logits, for 32 about 44, is put together in LDS and ranked by counting.  Where ties make more than
 // kShort of them, the utterance is done by lists.  bf16, with lists in brackets: 128 utterances of 16 rows of 1025 for 16 winners
 // 8.6 us (12.0), of 4 rows for 4 5.3 (6.5); 2048 of 8 rows for 8 25 (33); 2048 of 16 rows of 128 for 16 53 (76).  Every wave counts for itself where
 // the bound is, which one or two rows do not repay: 4096 of one row of 1025 for 16 15.2 (11.5), 128 of two 7.5 (7.4).
-constexpr int kShort = 64, kShortWinners = 16, kShortRows = 3, kShortRow = kTile + 64;
+constexpr int kShort = 128, kShortWinners = 32, kShortLeast = 3, kShortMost = 2 * kJoinWaves, kShortRow = kTile + 64;
 struct Candidate {
     u64 key, sub;          // the score's place in the order of doubles; hypothesis (complement), logit's place, token (complement)
     __device__ __forceinline__ bool above(const Candidate &o) const { return key > o.key || (key == o.key && sub > o.sub); }
@@ -415,7 +415,8 @@ __device__ __forceinline__ u64 score_key(double t)
     return t > -INFINITY ? (u >> 63 ? ~u : u | 0x8000000000000000ull) : 0;
 }
 
-template <int TYPE>
+// WIDTH: of the lists, where they are needed; ROWS: of a wave
+template <int TYPE, int WIDTH, int ROWS>
 __global__ void __launch_bounds__(kJoinWaves * 64)
 beam_short_kernel(const SelectArgs a)
 {
@@ -424,48 +425,59 @@ beam_short_kernel(const SelectArgs a)
     struct __attribute__((packed, aligned(sizeof(T)))) At { T e[PER]; };
     extern __shared__ __align__(16) unsigned char lds[];
     ShortLds &s = *reinterpret_cast<ShortLds *>(lds);
-    const int waves = blockDim.x >> 6, k = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, b = blockIdx.x, n = a.n_out;
-    const bool has_row = k < a.beams, full = a.V >= kTile;
-    const long long hyp = (long long)b * a.beams + (has_row ? k : 0);
-    const T *row = static_cast<const T *>(a.logits) + b * a.batch_stride + (has_row ? k : 0) * a.beam_stride;
-    // the row's logits, 17 a lane; `place`: where in the row
-    float f[ALL];
-    if (full) {
-        At v[LOADS];
+    const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, b = blockIdx.x, n = a.n_out;
+    const bool full = a.V >= kTile;
+    // the rows' logits, 17 a lane; `place`: where in the row
+    float f[ROWS][ALL], scores[ROWS];
+    bool ended[ROWS], live[ROWS];
 #pragma unroll
-        for (int q = 0; q < LOADS; ++q) v[q] = *reinterpret_cast<const At *>(row + (q * 64 + lane) * PER);
-        const T more = row[min(kTile + lane, a.V - 1)];
+    for (int r = 0; r < ROWS; ++r) {
+        const int k = wave + r * waves;
+        const bool has_row = k < a.beams;
+        const long long hyp = (long long)b * a.beams + (has_row ? k : 0);
+        const T *row = static_cast<const T *>(a.logits) + b * a.batch_stride + (has_row ? k : 0) * a.beam_stride;
+        if (full) {
+            At v[LOADS];
 #pragma unroll
-        for (int i = 0; i < ALL - 1; ++i) f[i] = (float)v[i / PER].e[i % PER];
-        f[ALL - 1] = kTile + lane < a.V ? (float)more : -INFINITY;
-    } else {
-        T v[ALL - 1];
+            for (int q = 0; q < LOADS; ++q) v[q] = *reinterpret_cast<const At *>(row + (q * 64 + lane) * PER);
+            const T more = row[min(kTile + lane, a.V - 1)];
 #pragma unroll
-        for (int i = 0; i < ALL - 1; ++i) v[i] = row[min(i * 64 + lane, a.V - 1)];
+            for (int i = 0; i < ALL - 1; ++i) f[r][i] = (float)v[i / PER].e[i % PER];
+            f[r][ALL - 1] = kTile + lane < a.V ? (float)more : -INFINITY;
+        } else {
+            T v[ALL - 1];
 #pragma unroll
-        for (int i = 0; i < ALL - 1; ++i) f[i] = i * 64 + lane < a.V ? (float)v[i] : -INFINITY;
-        f[ALL - 1] = -INFINITY;
+            for (int i = 0; i < ALL - 1; ++i) v[i] = row[min(i * 64 + lane, a.V - 1)];
+#pragma unroll
+            for (int i = 0; i < ALL - 1; ++i) f[r][i] = i * 64 + lane < a.V ? (float)v[i] : -INFINITY;
+            f[r][ALL - 1] = -INFINITY;
+        }
+        scores[r] = a.scores[hyp];
+        ended[r] = has_row && a.finished && a.finished[hyp];
+        live[r] = has_row && !ended[r] && scores[r] > -INFINITY;
     }
     auto place = [&](int i) { return !full ? i * 64 + lane : i < ALL - 1 ? (i / PER * 64 + lane) * PER + i % PER : kTile + lane; };
-    const float score = a.scores[hyp];
-    const bool ended = has_row && a.finished && a.finished[hyp], live = has_row && !ended && score > -INFINITY;
-    if (k == 0) { s.group[lane] = 0; if (lane == 0) s.count = 0; }
-    float m = f[0];
+    if (wave == 0) { s.group[lane] = 0; if (lane == 0) s.count = 0; }
+    float m[ROWS], top[ROWS];
+    double base[ROWS];
+    auto total = [&](int r, float x) { return base[r] + ((double)x - (double)top[r]); };
 #pragma unroll
-    for (int i = 1; i < ALL; ++i) m = fmaxf(m, f[i]);
-    const float top = fmaxf(wave_max(m), kLowest);
-    // (differences to the largest logit: at the ends of the type, too)
-    float part[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < ROWS; ++r) {
+        m[r] = f[r][0];
 #pragma unroll
-    for (int i = 0; i < ALL; ++i) part[i % 4] += __builtin_amdgcn_exp2f((f[i] - top) * kLog2E);
-    const double sum = wave_sum((double)((part[0] + part[1]) + (part[2] + part[3])));
-    const double base = (double)score - log(sum);          // (NaN where the row holds a NaN or an infinity)
-    auto total = [&](float x) { return base + ((double)x - (double)top); };
-    __syncthreads();                                       // (the cleared LDS)
-    if (live && m > -INFINITY) {
-        const double t = total(m);
-        if (t > -INFINITY) atomicMax(&s.group[lane], float_key((float)t));
+        for (int i = 1; i < ALL; ++i) m[r] = fmaxf(m[r], f[r][i]);
+        top[r] = fmaxf(wave_max(m[r]), kLowest);
+        // (differences to the largest logit: at the ends of the type, too)
+        float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < ALL; ++i) part[i % 4] += __builtin_amdgcn_exp2f((f[r][i] - top[r]) * kLog2E);
+        base[r] = (double)scores[r] - log(wave_sum((double)((part[0] + part[1]) + (part[2] + part[3]))));      // (NaN where the row holds a NaN or an infinity)
     }
+    __syncthreads();                                       // (the cleared LDS)
+    double t = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) if (live[r] && m[r] > -INFINITY && base[r] == base[r]) t = fmax(t, total(r, m[r]));
+    if (t > -INFINITY) atomicMax(&s.group[lane], float_key((float)t));
     __syncthreads();
     // the n-th of the lanes' largest
     const unsigned best = s.group[lane];
@@ -476,43 +488,44 @@ beam_short_kernel(const SelectArgs a)
         if (__popcll(__ballot(best >= with)) >= n) nth = with;
     }
     const float bar = key_float(nth);
-    // In the row's logits, and lower by more than all these roundings are off: logits from there on are candidates.
-    const double at = (double)bar - base + (double)top;
-    const float low = at == at ? (float)(at - (fabs(at) + fabs((double)bar) + fabs((double)top)) * 1e-6 - 1e-5) : -INFINITY;
-    u64 in[ALL];
-    int mine = 0;
 #pragma unroll
-    for (int i = 0; i < ALL; ++i) { in[i] = live && base == base ? __ballot(f[i] >= low && f[i] > -INFINITY) : 0; mine += __popcll(in[i]); }
-    if (ended) mine = 1;
-    if (mine > 0) {
+    for (int r = 0; r < ROWS; ++r) {
+        // In the row's logits, and lower by more than all these roundings are off: logits from there on are candidates.
+        const double at = (double)bar - base[r] + (double)top[r];
+        const float low = at == at ? (float)(at - (fabs(at) + fabs((double)bar) + fabs((double)top[r])) * 1e-6 - 1e-5) : -INFINITY;
+        const int k = wave + r * waves;
+        u64 in[ALL];
+        int mine = 0;
+#pragma unroll
+        for (int i = 0; i < ALL; ++i) { in[i] = live[r] && base[r] == base[r] ? __ballot(f[r][i] >= low && f[r][i] > -INFINITY) : 0; mine += __popcll(in[i]); }
+        if (ended[r]) mine = 1;
+        if (mine == 0) continue;
         int from = 0;
         if (lane == 0) from = atomicAdd(&s.count, mine);
         from = __builtin_amdgcn_readfirstlane(from);
         auto put = [&](float x, int token, double t, int to) {
             if (to < kShort) s.found[to] = Candidate{score_key(t), (u64)(63 - k) << 58 | (row_key(x, 0) >> 32) << 26 | (u64)(0x3ffffff - token)};
         };
-        if (ended) { if (lane == 0) put(0.f, a.end_token, (double)score, from); }
-        else {
+        if (ended[r]) { if (lane == 0) put(0.f, a.end_token, (double)scores[r], from); continue; }
 #pragma unroll
-            for (int i = 0; i < ALL; ++i) {
-                if (in[i] == 0ull) continue;
-                if (in[i] >> lane & 1) put(f[i], place(i), total(f[i]), from + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(in[i] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)in[i], 0u)));
-                from += __popcll(in[i]);
-            }
+        for (int i = 0; i < ALL; ++i) {
+            if (in[i] == 0ull) continue;
+            if (in[i] >> lane & 1) put(f[r][i], place(i), total(r, f[r][i]), from + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(in[i] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)in[i], 0u)));
+            from += __popcll(in[i]);
         }
     }
     __syncthreads();
     const int count = s.count;
     if (count > kShort) {                                  // (the whole work-group)
         __syncthreads();
-        select_rows<TYPE, 16>(a, lds);
+        select_rows<TYPE, WIDTH>(a, lds);
         return;
     }
     // a wave ranks every waves-th candidate: how many are above it
-    const Candidate own = lane < count ? s.found[lane] : Candidate{0, 0};
-    for (int c = k; c < count; c += waves) {
+    const Candidate own[2] = {lane < count ? s.found[lane] : Candidate{0, 0}, lane + 64 < count ? s.found[lane + 64] : Candidate{0, 0}};
+    for (int c = wave; c < count; c += waves) {
         const Candidate it = s.found[c];
-        const int rank = __popcll(__ballot(own.above(it)));
+        const int rank = __popcll(__ballot(own[0].above(it))) + __popcll(__ballot(own[1].above(it)));
         if (lane == 0 && rank < n && it.key != 0) {
             const long long o = (long long)b * n + rank;
             const u64 u = it.key >> 63 ? it.key ^ 0x8000000000000000ull : ~it.key;
@@ -521,8 +534,8 @@ beam_short_kernel(const SelectArgs a)
             a.parents_out[o] = 63 - (int)(it.sub >> 58);
         }
     }
-    const int there = __popcll(__ballot(own.key != 0));
-    if (k == 0 && lane >= there && lane < n) {
+    const int there = __popcll(__ballot(own[0].key != 0)) + __popcll(__ballot(own[1].key != 0));
+    if (wave == 0 && lane >= there && lane < n) {
         const long long o = (long long)b * n + lane;
         a.scores_out[o] = -INFINITY; a.tokens_out[o] = -1; a.parents_out[o] = -1;
     }
@@ -573,9 +586,9 @@ beam_scan_kernel(const SelectArgs a)
 // different ones; the n-th of them bounds the n-th best from below, and what is not below it, for n = 8 about nine logits of four pieces, is the
 // list.  Where ties make more than 64 of them, the work-group does its pieces the other way.  Bound by memory, and by the exponentials behind it: 67 MB
 // of f16 logits (64 x 8 rows of 65535) 17.5 us (lists: 24), 14 without the sums and the list.
-constexpr int kHeld = 16, kHeldWinners = 16;
+constexpr int kHeld = 16, kHeldWinners = 32;
 template <class T> constexpr int held_size() { return kHeld * 64 * 16 / (int)sizeof(T); }
-template <int TYPE>
+template <int TYPE, int WIDTH>
 __global__ void __launch_bounds__(kScanWaves * 64, 4)
 beam_held_kernel(const SelectArgs a)
 {
@@ -658,17 +671,17 @@ beam_held_kernel(const SelectArgs a)
     __syncthreads();
     const int count = found_count;
     if (count > 64) {                                      // (the whole work-group)
-        scan_pieces<TYPE, 16>(a, lds);
+        scan_pieces<TYPE, WIDTH>(a, lds);
         return;
     }
     if (wave != 0) return;
     InRow v{lane < count ? found[lane] : 0};
-    if (count <= 16) sort_lanes<16>(v);
+    if (WIDTH == 16 && count <= 16) sort_lanes<16>(v);
     else {
         sort_lanes<64>(v);
-        v = v.template lane<16>().template lane<32>();     // the best 16, worst first, to lanes 0 .. 15
+        if constexpr (WIDTH == 16) v = v.template lane<16>().template lane<32>();     // the best 16, worst first, to lanes 0 .. 15
     }
-    store_piece(a, lds, lane, reverse<16>(v).key);
+    store_piece(a, lds, lane, reverse<WIDTH>(v).key);
 }
 template <int WIDTH>
 __global__ void __launch_bounds__(kJoinWaves * 64)
@@ -844,11 +857,12 @@ bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(
 
 // How a selection is cut up.  One launch, a work-group an utterance and a wave a row, where that leaves a wave no more than
 // kOneLaunchTiles tiles: the second launch costs what a wave takes for several tiles.  Else pieces of two tiles or more, towards sixteen waves on
-// every compute unit.  Pieces that waves hold are read at the rate of memory however many there are: of few rows they pay from kFewTiles
-// on, and no number of rows is too large for them; lists are made in one launch where there are kWavesWanted rows.  us, one launch and two: 64 x 16
-// rows of 8000 bf16 logits for 16 winners 28.1 and 14.1, 64 x 4 of 5000 fp32 for 4 11.9 and 8.7, but 128 x 4 of 2049 fp32 for 4 8.4 and 9.0,
-// 128 x 16 of 4097 bf16 for 16 20.2 and 22.5, 1024 x 4 of 4097 for 4 17.7 and 30; 512 x 4 of 65537 for 4 69 (lists) and 54.
-constexpr int kOneLaunchTiles = 8, kFewTiles = 4, kFewRows = 2048, kWavesWanted = 4096, kMostPieces = 64 / kScanWaves;
+// every compute unit.  Pieces that waves hold are read at the rate of memory however many there are: of fewer than kWavesWanted rows they pay beyond
+// kFewTiles, and no number of rows is too large for them; lists are made in one launch from kWavesWanted rows on.  us, one launch and two: 64 x 16
+// rows of 8000 bf16 logits for 16 winners 28.1 and 14.1, 128 x 16 for 32 34.3 and 22.5, 8 x 32 of 2000 for 32 32.2 and 14.7, 8 x 8 of 3000 for 8 11.4 and 9.1,
+// but 128 x 4 of 2049 fp32 for 4 8.4 and 9.0, 100 x 16 of 2000 for 16 15.8 and 17.0, 128 x 16 of 4097 for 16 19.6 and 22.9, 1024 x 4 of 4097 for 4 17.7
+// and 30; 512 x 4 of 65537 for 4 69 (lists) and 54.
+constexpr int kOneLaunchTiles = 8, kFewTiles = 2, kWavesWanted = 4096, kMostPieces = 64 / kScanWaves;
 
 struct SelectPlan {
     bool two = false, is_short = false, held = false;
@@ -859,12 +873,12 @@ struct SelectPlan {
     {
         const int row = (V - 1) / kTile + 1;
         while (waves < kJoinWaves && waves < beams) waves *= 2;
-        is_short = V <= kShortRow && beams >= kShortRows && beams <= kJoinWaves && n <= kShortWinners;
+        is_short = V <= kShortRow && beams >= kShortLeast && beams <= kShortMost && n <= kShortWinners;
         lds = std::max(join_lds(waves, beams, n), is_short ? sizeof(ShortLds) : 0);
         // (rows that waves hold as a whole: in no more pieces than the join takes)
         const int most = (type == RNNT_TYPE_F32 ? held_size<float>() : held_size<__bf16>()) / kTile;
         held = n <= kHeldWinners && V >= 8 && (row + most * kScanWaves - 1) / (most * kScanWaves) <= kMostPieces;
-        if ((beams + waves - 1) / waves * row <= (held && B * beams < kFewRows ? kFewTiles : kOneLaunchTiles) || (!held && B * beams >= kWavesWanted)) return;
+        if (is_short || (beams + waves - 1) / waves * row <= (held && B * beams < kWavesWanted ? kFewTiles : kOneLaunchTiles) || (!held && B * beams >= kWavesWanted)) return;
         two = true;
         const int64_t into = std::min<int64_t>(std::max<int64_t>(kWavesWanted / (B * beams * kScanWaves), 1), std::min(kMostPieces, (row + 2 * kScanWaves - 1) / (2 * kScanWaves)));
         piece_tiles = (int)((row + into * kScanWaves - 1) / (into * kScanWaves));
@@ -911,7 +925,9 @@ int rnnt_beam_select(const void *logits, int32_t type, int64_t batch_stride, int
     if (!p.two) {
         auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(B), dim3(p.waves * 64), (unsigned)p.lds, on, args); };
         auto with = [&](auto t) {
-            if (p.is_short) run(beam_short_kernel<t()>);
+            if (p.is_short && p.waves < beams) run(beam_short_kernel<t(), 64, 2>);
+            else if (p.is_short && n_out <= 16) run(beam_short_kernel<t(), 16, 1>);
+            else if (p.is_short) run(beam_short_kernel<t(), 64, 1>);
             else if (n_out <= 16) run(beam_select_kernel<t(), 16>);
             else run(beam_select_kernel<t(), 64>);
         };
@@ -928,7 +944,8 @@ int rnnt_beam_select(const void *logits, int32_t type, int64_t batch_stride, int
     args.refs = args.sums + n * kScanWaves;
     auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(kScanWaves * 64), 0, on, args); };
     auto with = [&](auto t) {
-        if (p.held) run(beam_held_kernel<t()>);
+        if (p.held && n_out <= 16) run(beam_held_kernel<t(), 16>);
+        else if (p.held) run(beam_held_kernel<t(), 64>);
         else if (n_out <= 16) run(beam_scan_kernel<t(), 16>);
         else run(beam_scan_kernel<t(), 64>);
     };

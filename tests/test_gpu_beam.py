@@ -33,7 +33,8 @@ def _check(pkg, x, scores, n, finished=None, end=0):  # noqa: F811
 
 CASES = [(1, 1, 1, 1), (1, 1, 5, 5), (2, 3, 7, 9), (1, 4, 1025, 4), (3, 8, 1025, 8), (2, 16, 257, 16), (5, 5, 64, 3), (1, 64, 130, 64), (2, 33, 1000, 33),
          (1, 2, 4096, 64), (2, 4, 8193, 10), (1, 1, 65535, 64), (3, 7, 20001, 12), (1, 64, 20000, 64), (130, 2, 100, 2), (1, 3, 3, 20),
-         (1, 2, 8192, 5), (2, 1, 32769, 16), (3, 2, 65543, 4), (1, 1, 262145, 8), (1, 1, 524289, 3), (1050, 2, 9001, 2), (40, 30, 1030, 7)]
+         (1, 2, 8192, 5), (2, 1, 32769, 16), (3, 2, 65543, 4), (1, 1, 262145, 8), (1, 1, 524289, 3), (1050, 2, 9001, 2), (40, 30, 1030, 7),
+         (3, 2, 9000, 32), (1, 3, 70000, 25), (2, 32, 3000, 32), (2, 3, 9000, 33), (4200, 1, 9000, 40)]
 
 
 @pytest.mark.parametrize("B,beams,V,n", CASES)
@@ -73,7 +74,8 @@ def test_ties_go_to_the_lowest_place(pkg, V, n):  # noqa: F811
 
 
 @pytest.mark.parametrize("B,beams,V,n", [(2, 3, 1, 2), (3, 16, 1, 16), (2, 4, 63, 16), (3, 7, 1023, 11), (3, 16, 1024, 16), (2, 5, 1025, 1), (2, 16, 1087, 16),
-                                         (2, 15, 1088, 16), (2, 16, 1089, 16), (2, 16, 1025, 17), (2, 17, 1025, 16), (300, 3, 40, 5)])
+                                         (2, 15, 1088, 16), (2, 16, 1089, 16), (2, 16, 1025, 17), (2, 17, 1025, 16), (300, 3, 40, 5),
+                                         (2, 32, 1025, 32), (2, 31, 300, 20), (3, 4, 1088, 33), (2, 33, 1025, 32), (2, 20, 1024, 5), (2, 3, 500, 32)])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_short_rows(pkg, B, beams, V, n, dtype):  # noqa: F811
     """Around the lengths, hypotheses and winners up to which rows are short: random logits, few different ones, all the
