@@ -415,6 +415,60 @@ __device__ __forceinline__ u64 score_key(double t)
     return t > -INFINITY ? (u >> 63 ? ~u : u | 0x8000000000000000ull) : 0;
 }
 
+// The n-th of the lanes' largest scores, rounded down
+__device__ __forceinline__ float score_bar(const ShortLds &s, int lane, int n)
+{
+    const unsigned best = s.group[lane];
+    unsigned nth = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 8; --bit) {
+        const unsigned with = nth | 1u << bit;
+        if (__popcll(__ballot(best >= with)) >= n) nth = with;
+    }
+    return key_float(nth);
+}
+// It in the logits of a row whose scores are base + (logit - ref), and lower by more than all these roundings are off: logits from there on are candidates.
+__device__ __forceinline__ float logit_bar(float bar, double base, double ref)
+{
+    const double at = (double)bar - base + ref;
+    return at == at ? fmaxf((float)(at - (fabs(at) + fabs((double)bar) + fabs(ref)) * 1e-6 - 1e-5), kLowest) : kLowest;
+}
+__device__ __forceinline__ void put_candidate(ShortLds &s, int to, int k, float x, int token, double score)
+{
+    if (to < kShort) s.found[to] = Candidate{score_key(score), (u64)(63 - k) << 58 | (row_key(x, 0) >> 32) << 26 | (u64)(0x3ffffff - token)};
+}
+// What the waves have put together, or, where that is too much, the utterance by lists
+template <int TYPE, int WIDTH>
+__device__ __forceinline__ void rank_candidates(const SelectArgs &a, ShortLds &s, unsigned char *lds)
+{
+    const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, b = blockIdx.x, n = a.n_out;
+    __syncthreads();
+    const int count = s.count;
+    if (count > kShort) {                                  // (the whole work-group)
+        __syncthreads();
+        select_rows<TYPE, WIDTH>(a, lds);
+        return;
+    }
+    // a wave ranks every waves-th candidate: how many are above it
+    const Candidate own[2] = {lane < count ? s.found[lane] : Candidate{0, 0}, lane + 64 < count ? s.found[lane + 64] : Candidate{0, 0}};
+    for (int c = wave; c < count; c += waves) {
+        const Candidate it = s.found[c];
+        const int rank = __popcll(__ballot(own[0].above(it))) + __popcll(__ballot(own[1].above(it)));
+        if (lane == 0 && rank < n && it.key != 0) {
+            const long long o = (long long)b * n + rank;
+            const u64 u = it.key >> 63 ? it.key ^ 0x8000000000000000ull : ~it.key;
+            a.scores_out[o] = (float)__builtin_bit_cast(double, u);
+            a.tokens_out[o] = 0x3ffffff - (int)(it.sub & 0x3ffffff);
+            a.parents_out[o] = 63 - (int)(it.sub >> 58);
+        }
+    }
+    const int there = __popcll(__ballot(own[0].key != 0)) + __popcll(__ballot(own[1].key != 0));
+    if (wave == 0 && lane >= there && lane < n) {
+        const long long o = (long long)b * n + lane;
+        a.scores_out[o] = -INFINITY; a.tokens_out[o] = -1; a.parents_out[o] = -1;
+    }
+}
+
 // WIDTH: of the lists, where they are needed; ROWS: of a wave
 template <int TYPE, int WIDTH, int ROWS>
 __global__ void __launch_bounds__(kJoinWaves * 64)
@@ -479,66 +533,156 @@ beam_short_kernel(const SelectArgs a)
     for (int r = 0; r < ROWS; ++r) if (live[r] && m[r] > -INFINITY && base[r] == base[r]) t = fmax(t, total(r, m[r]));
     if (t > -INFINITY) atomicMax(&s.group[lane], float_key((float)t));
     __syncthreads();
-    // the n-th of the lanes' largest
-    const unsigned best = s.group[lane];
-    unsigned nth = 0;
-#pragma unroll
-    for (int bit = 31; bit >= 8; --bit) {
-        const unsigned with = nth | 1u << bit;
-        if (__popcll(__ballot(best >= with)) >= n) nth = with;
-    }
-    const float bar = key_float(nth);
+    const float bar = score_bar(s, lane, n);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-        // In the row's logits, and lower by more than all these roundings are off: logits from there on are candidates.
-        const double at = (double)bar - base[r] + (double)top[r];
-        const float low = at == at ? (float)(at - (fabs(at) + fabs((double)bar) + fabs((double)top[r])) * 1e-6 - 1e-5) : -INFINITY;
+        const float low = logit_bar(bar, base[r], (double)top[r]);
         const int k = wave + r * waves;
         u64 in[ALL];
         int mine = 0;
 #pragma unroll
-        for (int i = 0; i < ALL; ++i) { in[i] = live[r] && base[r] == base[r] ? __ballot(f[r][i] >= low && f[r][i] > -INFINITY) : 0; mine += __popcll(in[i]); }
+        for (int i = 0; i < ALL; ++i) { in[i] = live[r] && base[r] == base[r] ? __ballot(f[r][i] >= low) : 0; mine += __popcll(in[i]); }
         if (ended[r]) mine = 1;
         if (mine == 0) continue;
         int from = 0;
         if (lane == 0) from = atomicAdd(&s.count, mine);
         from = __builtin_amdgcn_readfirstlane(from);
-        auto put = [&](float x, int token, double t, int to) {
-            if (to < kShort) s.found[to] = Candidate{score_key(t), (u64)(63 - k) << 58 | (row_key(x, 0) >> 32) << 26 | (u64)(0x3ffffff - token)};
-        };
-        if (ended[r]) { if (lane == 0) put(0.f, a.end_token, (double)scores[r], from); continue; }
+        if (ended[r]) { if (lane == 0) put_candidate(s, from, k, 0.f, a.end_token, (double)scores[r]); continue; }
 #pragma unroll
         for (int i = 0; i < ALL; ++i) {
             if (in[i] == 0ull) continue;
-            if (in[i] >> lane & 1) put(f[r][i], place(i), total(r, f[r][i]), from + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(in[i] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)in[i], 0u)));
+            if (in[i] >> lane & 1)
+                put_candidate(s, from + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(in[i] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)in[i], 0u)), k, f[r][i], place(i), total(r, f[r][i]));
             from += __popcll(in[i]);
         }
     }
-    __syncthreads();
-    const int count = s.count;
-    if (count > kShort) {                                  // (the whole work-group)
-        __syncthreads();
-        select_rows<TYPE, WIDTH>(a, lds);
-        return;
+    rank_candidates<TYPE, WIDTH>(a, s, lds);
+}
+
+// A row or a piece of one that a wave holds as a whole, kHeld loads a lane
+constexpr int kHeld = 16, kHeldWinners = 32;
+template <class T> constexpr int held_size() { return kHeld * 64 * 16 / (int)sizeof(T); }
+template <class T> struct Held {
+    static constexpr int PER = 16 / (int)sizeof(T);
+    struct __attribute__((packed, aligned(sizeof(T)))) At { T e[PER]; };
+    const T *row;
+    int rest, lane;
+    At held[kHeld];
+    float most[kHeld], m;          // the lane's largest of each load, and of all
+    double sum, ref;               // the wave's, of exp(x - ref)
+    // A load that would go on behind the end is the last one before it (a row has PER logits or more); `twice`
+    // of its logits are another load's, or another wave's.
+    __device__ __forceinline__ int off(int q) const { return min((q * 64 + lane) * PER, rest - PER); }
+    __device__ __forceinline__ void load()
+    {
+#pragma unroll
+        for (int q = 0; q < kHeld; ++q) held[q] = *reinterpret_cast<const At *>(row + off(q));
     }
-    // a wave ranks every waves-th candidate: how many are above it
-    const Candidate own[2] = {lane < count ? s.found[lane] : Candidate{0, 0}, lane + 64 < count ? s.found[lane + 64] : Candidate{0, 0}};
-    for (int c = wave; c < count; c += waves) {
-        const Candidate it = s.found[c];
-        const int rank = __popcll(__ballot(own[0].above(it))) + __popcll(__ballot(own[1].above(it)));
-        if (lane == 0 && rank < n && it.key != 0) {
-            const long long o = (long long)b * n + rank;
-            const u64 u = it.key >> 63 ? it.key ^ 0x8000000000000000ull : ~it.key;
-            a.scores_out[o] = (float)__builtin_bit_cast(double, u);
-            a.tokens_out[o] = 0x3ffffff - (int)(it.sub & 0x3ffffff);
-            a.parents_out[o] = 63 - (int)(it.sub >> 58);
+    // (a lane's running maximum and sum, as in Scan, sixteen logits at a time: made while others are on their way)
+    __device__ __forceinline__ void add_up()
+    {
+        constexpr int LOADS = 16 / PER;
+        float shift = kLowest;
+        m = -INFINITY;
+        sum = 0;
+#pragma unroll
+        for (int q0 = 0; q0 < kHeld; q0 += LOADS) {
+#pragma unroll
+            for (int q = q0; q < q0 + LOADS; ++q) {
+                most[q] = -INFINITY;
+                if (q * 64 * PER >= rest) continue;
+                if ((q + 1) * 64 * PER > rest) {
+                    const int twice = (q * 64 + lane) * PER - off(q);
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) if (e < twice) held[q].e[e] = (T)-INFINITY;
+                }
+#pragma unroll
+                for (int e = 0; e < PER; ++e) most[q] = fmaxf(most[q], (float)held[q].e[e]);
+                m = fmaxf(m, most[q]);
+            }
+            if (q0 * 64 * PER >= rest) continue;
+            const float now = fmaxf(m * kLog2E, kLeast);
+            float part[2] = {0.f, 0.f};
+#pragma unroll
+            for (int q = q0; q < q0 + LOADS; ++q) {
+                if (q * 64 * PER >= rest) continue;
+#pragma unroll
+                for (int e = 0; e < PER; ++e) part[e % 2] += __builtin_amdgcn_exp2f(__builtin_fmaf((float)held[q].e[e], kLog2E, -now));
+            }
+            sum = sum * (double)__builtin_amdgcn_exp2f(shift - now) + (double)(part[0] + part[1]);
+            shift = now;
+        }
+        const float top = wave_max(fmaxf(m, kLowest));
+        if (!(fabsf(top) < kFar)) {
+            sum = 0;
+#pragma unroll 1
+            for (int j = lane; j < rest; j += 64) sum += (double)__builtin_amdgcn_exp2f(((float)row[j] - top) * kLog2E);
+            sum = wave_sum(sum);
+            ref = (double)top;
+            return;
+        }
+        const float all = wave_max(shift);
+        sum = wave_sum(sum * (double)__builtin_amdgcn_exp2f(shift - all));
+        ref = (double)all / (double)kLog2E;
+    }
+    // put(logit, place) for each logit from `low` on
+    template <class Put> __device__ __forceinline__ void each(float low, Put &&put)
+    {
+        // (widened anew: kept, they would take twice the registers)
+#pragma unroll
+        for (int q = 0; q < kHeld; ++q) {
+            v4u raw = __builtin_bit_cast(v4u, held[q]);
+            asm volatile("" : "+v"(raw));
+            held[q] = __builtin_bit_cast(At, raw);
+        }
+#pragma unroll
+        for (int q = 0; q < kHeld; ++q) {
+            if (__ballot(most[q] >= low) == 0ull) continue;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                const float x = (float)held[q].e[e];
+                if (x >= low) put(x, off(q) + e);
+            }
         }
     }
-    const int there = __popcll(__ballot(own[0].key != 0)) + __popcll(__ballot(own[1].key != 0));
-    if (wave == 0 && lane >= there && lane < n) {
-        const long long o = (long long)b * n + lane;
-        a.scores_out[o] = -INFINITY; a.tokens_out[o] = -1; a.parents_out[o] = -1;
+};
+
+// Rows of a few tiles, one for each wave, the way of the short ones
+template <int TYPE, int WIDTH>
+__global__ void __launch_bounds__(kJoinWaves * 64)
+beam_row_kernel(const SelectArgs a)
+{
+    typedef typename Logit<TYPE>::T T;
+    extern __shared__ __align__(16) unsigned char lds[];
+    ShortLds &s = *reinterpret_cast<ShortLds *>(lds);
+    const int k = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, b = blockIdx.x;
+    const bool has_row = k < a.beams;
+    const long long hyp = (long long)b * a.beams + (has_row ? k : 0);
+    Held<T> h;
+    h.row = static_cast<const T *>(a.logits) + b * a.batch_stride + (has_row ? k : 0) * a.beam_stride;
+    h.rest = a.V;
+    h.lane = lane;
+    h.load();
+    const float score = a.scores[hyp];
+    const bool ended = has_row && a.finished && a.finished[hyp], live = has_row && !ended && score > -INFINITY;
+    if (k == 0) { s.group[lane] = 0; if (lane == 0) s.count = 0; }
+    double base = 0;
+    if (live) {
+        h.add_up();
+        base = (double)score - log(h.sum);                 // (NaN where the row holds a NaN or an infinity)
     }
+    auto total = [&](float x) { return base + ((double)x - h.ref); };
+    const bool good = live && base == base;
+    __syncthreads();                                       // (the cleared LDS)
+    if (good && h.m > -INFINITY) {
+        const double t = total(h.m);
+        if (t > -INFINITY) atomicMax(&s.group[lane], float_key((float)t));
+    }
+    __syncthreads();
+    const float low = logit_bar(score_bar(s, lane, a.n_out), base, h.ref);
+    if (good) h.each(low, [&](float x, int token) { put_candidate(s, atomicAdd(&s.count, 1), k, x, token, total(x)); });
+    if (ended && lane == 0) put_candidate(s, atomicAdd(&s.count, 1), k, 0.f, a.end_token, (double)score);
+    rank_candidates<TYPE, WIDTH>(a, s, lds);
 }
 
 // Long rows: pieces over the whole device, joined by a second launch.  A work-group's waves have four pieces
@@ -585,89 +729,38 @@ beam_scan_kernel(const SelectArgs a)
 // The same for few winners and pieces that a wave holds as a whole, kHeld loads a lane.  The lanes' largest logits in the four pieces are 64
 // different ones; the n-th of them bounds the n-th best from below, and what is not below it, for n = 8 about nine logits of four pieces, is the
 // list.  Where ties make more than 64 of them, the work-group does its pieces the other way.  Bound by memory, and by the exponentials behind it: 67 MB
-// of f16 logits (64 x 8 rows of 65535) 17.5 us (lists: 24), 14 without the sums and the list.
-constexpr int kHeld = 16, kHeldWinners = 32;
-template <class T> constexpr int held_size() { return kHeld * 64 * 16 / (int)sizeof(T); }
+// of f16 logits (64 x 8 rows of 65535) 18 us (lists: 24), 14 without the sums and the list.
 template <int TYPE, int WIDTH>
 __global__ void __launch_bounds__(kScanWaves * 64, 4)
 beam_held_kernel(const SelectArgs a)
 {
     typedef typename Logit<TYPE>::T T;
-    constexpr int PER = 16 / (int)sizeof(T);
-    struct __attribute__((packed, aligned(sizeof(T)))) At { T e[PER]; };
     __shared__ ScanLds lds;
     __shared__ u64 found[64];
     __shared__ unsigned group[64];
     __shared__ int found_count;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const Piece p = piece_of(a, wave);
-    const int rest = p.to - p.from;
-    const T *row = static_cast<const T *>(a.logits) + p.b * a.batch_stride + (p.hyp - p.b * a.beams) * a.beam_stride + p.from;
-    // A load that would go on behind the piece's end is the last one before it (a row has PER logits or more); `twice`
-    // of its logits are another load's, or another wave's.
-    auto off = [&](int q) { return min((q * 64 + lane) * PER, rest - PER); };
-    At held[kHeld];
-#pragma unroll
-    for (int q = 0; q < kHeld; ++q) held[q] = *reinterpret_cast<const At *>(row + off(q));
+    Held<T> h;
+    h.row = static_cast<const T *>(a.logits) + p.b * a.batch_stride + (p.hyp - p.b * a.beams) * a.beam_stride + p.from;
+    h.rest = p.to - p.from;
+    h.lane = lane;
+    h.load();
     if ((a.finished && a.finished[p.hyp]) || !(a.scores[p.hyp] > -INFINITY)) return;       // (the whole work-group)
     if (wave == 0) { group[lane] = 0; if (lane == 0) found_count = 0; }
-    // The sum is of differences to the largest logit of the first load, so that it is made while others are on their way; where that
-    // turns out to be far from the largest one of all, it is made again.
-    float most[kHeld], m = -INFINITY, now = 0.f, first = kLowest, part[2] = {0.f, 0.f};
-    double sum = 0, ref;
-#pragma unroll
-    for (int q = 0; q < kHeld; ++q) {
-        most[q] = -INFINITY;
-        if (q * 64 * PER >= rest) continue;
-        if ((q + 1) * 64 * PER > rest) {
-            const int twice = (q * 64 + lane) * PER - off(q);
-#pragma unroll
-            for (int e = 0; e < PER; ++e) if (e < twice) held[q].e[e] = (T)-INFINITY;
-        }
-#pragma unroll
-        for (int e = 0; e < PER; ++e) most[q] = fmaxf(most[q], (float)held[q].e[e]);
-        m = fmaxf(m, most[q]);
-        if (q == 0) { first = wave_max(fmaxf(m, kLowest)); now = first * kLog2E; }
-#pragma unroll
-        for (int e = 0; e < PER; ++e) part[e % 2] += __builtin_amdgcn_exp2f(__builtin_fmaf((float)held[q].e[e], kLog2E, -now));
-        if ((q + 1) * PER % 16 == 0 || (q + 1) * 64 * PER >= rest) { sum += (double)(part[0] + part[1]); part[0] = part[1] = 0.f; }
-    }
-    const float top = wave_max(fmaxf(m, kLowest));
-    if (!(top - first < 60.f) || !(fabsf(first) < kFar)) {
-        sum = 0;
-#pragma unroll 1
-        for (int j = lane; j < rest; j += 64) sum += (double)__builtin_amdgcn_exp2f(((float)row[j] - top) * kLog2E);
-        ref = (double)top;
-    } else ref = (double)now / (double)kLog2E;
-    sum = wave_sum(sum);
-    if (lane == 0) { lds.sums[wave] = sum; lds.refs[wave] = ref; }
+    h.add_up();
+    if (lane == 0) { lds.sums[wave] = h.sum; lds.refs[wave] = h.ref; }
     __syncthreads();                                       // (the cleared LDS)
-    if (m > -INFINITY) atomicMax(&group[lane], (unsigned)(row_key(m, 0) >> 32));
+    if (h.m > -INFINITY) atomicMax(&group[lane], (unsigned)(row_key(h.m, 0) >> 32));
     __syncthreads();
     const unsigned best = group[lane];
     unsigned nth = 0;                                      // (its highest 20 bits: from a little lower on)
 #pragma unroll
     for (int bit = 31; bit >= 12; --bit) if (__popcll(__ballot(best >= (nth | 1u << bit))) >= a.n_out) nth |= 1u << bit;
-    const float low = fmaxf(key_logit((u64)nth << 32), kLowest);
-    // (widened anew: kept, they would take twice the registers)
-#pragma unroll
-    for (int q = 0; q < kHeld; ++q) {
-        v4u raw = __builtin_bit_cast(v4u, held[q]);
-        asm volatile("" : "+v"(raw));
-        held[q] = __builtin_bit_cast(At, raw);
-    }
-#pragma unroll
-    for (int q = 0; q < kHeld; ++q) {
-        if (__ballot(most[q] >= low) == 0ull) continue;
-#pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            const float x = (float)held[q].e[e];
-            if (x >= low) {
-                const int at = atomicAdd(&found_count, 1);
-                if (at < 64) found[at] = row_key(x, p.from + off(q) + e);
-            }
-        }
-    }
+    h.each(fmaxf(key_logit((u64)nth << 32), kLowest), [&](float x, int token) {
+        const int at = atomicAdd(&found_count, 1);
+        if (at < 64) found[at] = row_key(x, p.from + token);
+    });
     __syncthreads();
     const int count = found_count;
     if (count > 64) {                                      // (the whole work-group)
@@ -855,17 +948,19 @@ namespace {
 constexpr int64_t kMostThreads = 0xffffffff;                                // of a launch, at most
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
-// How a selection is cut up.  One launch, a work-group an utterance and a wave a row, where that leaves a wave no more than
-// kOneLaunchTiles tiles: the second launch costs what a wave takes for several tiles.  Else pieces of two tiles or more, towards sixteen waves on
-// every compute unit.  Pieces that waves hold are read at the rate of memory however many there are: of fewer than kWavesWanted rows they pay beyond
-// kFewTiles, and no number of rows is too large for them; lists are made in one launch from kWavesWanted rows on.  us, one launch and two: 64 x 16
-// rows of 8000 bf16 logits for 16 winners 28.1 and 14.1, 128 x 16 for 32 34.3 and 22.5, 8 x 32 of 2000 for 32 32.2 and 14.7, 8 x 8 of 3000 for 8 11.4 and 9.1,
-// but 128 x 4 of 2049 fp32 for 4 8.4 and 9.0, 100 x 16 of 2000 for 16 15.8 and 17.0, 128 x 16 of 4097 for 16 19.6 and 22.9, 1024 x 4 of 4097 for 4 17.7
-// and 30; 512 x 4 of 65537 for 4 69 (lists) and 54.
-constexpr int kOneLaunchTiles = 8, kFewTiles = 2, kWavesWanted = 4096, kMostPieces = 64 / kScanWaves;
+// How a selection is cut up.  One launch, a work-group an utterance: short rows; rows that a wave holds as a whole, where that leaves a work-group
+// no more than kOneRowTiles tiles or there are kOneRowRows rows, and its waves few winners to rank; and by lists, where a wave has no
+// more than kOneLaunchTiles tiles, of fewer than kWavesWanted rows that could be held in pieces kFewTiles: the second launch costs what a wave takes
+// for several tiles.  Else pieces of two tiles or more, towards sixteen waves on every compute unit; lists in pieces of fewer than kWavesWanted rows only.
+// us, bf16, rows held whole and in pieces: 1 x 4 rows of 4097 logits for 4 winners 7.5 and 8.7, 128 x 16 for 16 15.5 and 23, 1024 x 4 of 8192 for 4 18
+// and 26, 8 x 8 of 3000 for 8 8.7 and 9.1, but 16 x 16 of 4097 for 16 13.5 and 12.4, 64 x 16 of 8000 17.4 and 14.5, 1 x 2 of 3000 fp32 for 30 11.4 and 8.8,
+// 4096 x 2 of 1025 for 8 21.3 (lists 18.6).
+// By lists and in pieces: 128 x 20 of 4000 for 20 28.6 and 22.6, 8 x 32 of 2000 for 32 32 and 14.7, 512 x 4 of 65537 for 4 69 and 54, but
+// 128 x 32 of 2000 for 32 32 and 34.
+constexpr int kOneLaunchTiles = 8, kOneRowTiles = 64, kOneRowRows = 2048, kFewTiles = 2, kWavesWanted = 4096, kMostPieces = 64 / kScanWaves;
 
 struct SelectPlan {
-    bool two = false, is_short = false, held = false;
+    bool two = false, is_short = false, one_row = false, held = false;
     int pieces = 1, piece_tiles = 1, waves = 1;
     size_t lds = 0;
     int64_t bytes = 0;
@@ -874,11 +969,12 @@ struct SelectPlan {
         const int row = (V - 1) / kTile + 1;
         while (waves < kJoinWaves && waves < beams) waves *= 2;
         is_short = V <= kShortRow && beams >= kShortLeast && beams <= kShortMost && n <= kShortWinners;
-        lds = std::max(join_lds(waves, beams, n), is_short ? sizeof(ShortLds) : 0);
+        lds = std::max(join_lds(waves, beams, n), sizeof(ShortLds));
         // (rows that waves hold as a whole: in no more pieces than the join takes)
         const int most = (type == RNNT_TYPE_F32 ? held_size<float>() : held_size<__bf16>()) / kTile;
         held = n <= kHeldWinners && V >= 8 && (row + most * kScanWaves - 1) / (most * kScanWaves) <= kMostPieces;
-        if (is_short || (beams + waves - 1) / waves * row <= (held && B * beams < kWavesWanted ? kFewTiles : kOneLaunchTiles) || (!held && B * beams >= kWavesWanted)) return;
+        one_row = !is_short && held && row <= most && beams <= kJoinWaves && n <= waves * std::min(waves, 4) && (row * waves <= kOneRowTiles || B * beams >= kOneRowRows);
+        if (is_short || one_row || (beams + waves - 1) / waves * row <= (held && B * beams < kWavesWanted ? kFewTiles : kOneLaunchTiles) || (!held && B * beams >= kWavesWanted)) return;
         two = true;
         const int64_t into = std::min<int64_t>(std::max<int64_t>(kWavesWanted / (B * beams * kScanWaves), 1), std::min(kMostPieces, (row + 2 * kScanWaves - 1) / (2 * kScanWaves)));
         piece_tiles = (int)((row + into * kScanWaves - 1) / (into * kScanWaves));
@@ -925,7 +1021,9 @@ int rnnt_beam_select(const void *logits, int32_t type, int64_t batch_stride, int
     if (!p.two) {
         auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(B), dim3(p.waves * 64), (unsigned)p.lds, on, args); };
         auto with = [&](auto t) {
-            if (p.is_short && p.waves < beams) run(beam_short_kernel<t(), 64, 2>);
+            if (p.one_row && n_out <= 16) run(beam_row_kernel<t(), 16>);
+            else if (p.one_row) run(beam_row_kernel<t(), 64>);
+            else if (p.is_short && p.waves < beams) run(beam_short_kernel<t(), 64, 2>);
             else if (p.is_short && n_out <= 16) run(beam_short_kernel<t(), 16, 1>);
             else if (p.is_short) run(beam_short_kernel<t(), 64, 1>);
             else if (n_out <= 16) run(beam_select_kernel<t(), 16>);

@@ -75,10 +75,11 @@ def test_ties_go_to_the_lowest_place(pkg, V, n):  # noqa: F811
 
 @pytest.mark.parametrize("B,beams,V,n", [(2, 3, 1, 2), (3, 16, 1, 16), (2, 4, 63, 16), (3, 7, 1023, 11), (3, 16, 1024, 16), (2, 5, 1025, 1), (2, 16, 1087, 16),
                                          (2, 15, 1088, 16), (2, 16, 1089, 16), (2, 16, 1025, 17), (2, 17, 1025, 16), (300, 3, 40, 5),
-                                         (2, 32, 1025, 32), (2, 31, 300, 20), (3, 4, 1088, 33), (2, 33, 1025, 32), (2, 20, 1024, 5), (2, 3, 500, 32)])
+                                         (2, 32, 1025, 32), (2, 31, 300, 20), (3, 4, 1088, 33), (2, 33, 1025, 32), (2, 20, 1024, 5), (2, 3, 500, 32),
+                                         (3, 16, 4096, 16), (2, 8, 4097, 32), (2, 4, 8192, 16), (2, 5, 8000, 9), (2, 7, 1500, 12), (2, 8, 8193, 32), (260, 8, 3000, 4)])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_short_rows(pkg, B, beams, V, n, dtype):  # noqa: F811
-    """Around the lengths, hypotheses and winners up to which rows are short: random logits, few different ones, all the
+    """Around the lengths, hypotheses and winners up to which rows are short or held by one wave: random logits, few different ones, all the
     same but a few, masked ones, and magnitudes at which the scores lose the logits."""
     import torch
     g = torch.Generator().manual_seed(B + 10 * beams + V + n)
@@ -184,6 +185,19 @@ def test_long_rows_whose_first_logits_say_nothing(pkg, dtype):  # noqa: F811
     x[6, :, :700] = -low
     x[7, :, ::3] = -low / 2
     scores = -torch.rand((8, 2), generator=g)
+    _check(pkg, x.to(_torch_type(dtype)), scores, 9)
+
+
+@pytest.mark.parametrize("V", [700, 1025, 3000, 8000, 40000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_one_logit_above_the_others(pkg, V, dtype):  # noqa: F811
+    """By more and more, late in the row and early: what the terms of the sum are differences to is near their largest one."""
+    import torch
+    g = torch.Generator().manual_seed(V)
+    x = torch.randn((12, 3, V), generator=g)
+    for i in range(12):
+        x[i, 0, V - 10], x[i, 1, V // 3], x[i, 2, 5] = 4 + 1.3 * i, 5 + 7.1 * i, 3 + 2.7 * i
+    scores = -torch.rand((12, 3), generator=g)
     _check(pkg, x.to(_torch_type(dtype)), scores, 9)
 
 
