@@ -162,7 +162,7 @@ constexpr float kFar = 0x1p23f, kLeast = -0x1p24f;
 // logits.  A tile is 16 logits a lane (and 64 more where the row ends with them: vocabularies are a power of two and a blank).
 // A tile none of whose logits is above the n-th best so far goes by at the price of one comparison; of the others a lane
 // notes which of its own are, and one a lane at a time they go into a buffer, which is sorted and joined with the list 64 at a time.
-// (LONG: for many tiles; where the buffer has room they go there from the registers, 17 places in the code that are mostly skipped.
+// (LONG: for many tiles a wave; where the buffer has room they go there from the registers, 17 places in the code that are mostly skipped.
 // For a tile or two that costs more in instructions fetched than it saves: 4 rows of 1025 logits take 6.1 us with it and 5.6 without.)
 // Before there is a list, the maxima of n or more groups of lanes bound the n-th best from below.
 template <class T, int WIDTH, bool LONG> struct Scan {
@@ -667,6 +667,7 @@ beam_row_kernel(const SelectArgs a)
     const bool ended = has_row && a.finished && a.finished[hyp], live = has_row && !ended && score > -INFINITY;
     if (k == 0) { s.group[lane] = 0; if (lane == 0) s.count = 0; }
     double base = 0;
+    h.ref = 0;
     if (live) {
         h.add_up();
         base = (double)score - log(h.sum);                 // (NaN where the row holds a NaN or an infinity)
