@@ -148,7 +148,7 @@ def _products(pkg, M, N, K, a_type, y_type):  # noqa: F811
     assert torch.equal(again, got)
 
 
-@pytest.mark.parametrize("M,N,K", [(4099, 4100, 300), (8200, 2050, 1290), (4000, 8000, 128)])
+@pytest.mark.parametrize("M,N,K", [(4099, 4100, 300), (8200, 2050, 1290), (4000, 8000, 128), (4099, 4100, 129), (6200, 6200, 256), (6150, 6400, 520)])
 @pytest.mark.parametrize("a_type,y_type", [("mx4", "f32"), ("bf16", "bf16")])
 def test_large_products(pkg, M, N, K, a_type, y_type):  # noqa: F811
     """Sizes that the largest tiles are chosen for, with rows and columns that end inside one."""
