@@ -681,20 +681,20 @@ int rnnt_mx4_product(const void *a, const void *a_scales, int32_t a_type, int64_
         MX4_TRY(hipGetLastError());
         return RNNT_OK;
     }
-    if (!codes) {
-        int64_t cb = 0, sb = 0;
-        (void)rnnt_mx4_sizes(M, K, &cb, &sb);
-        unsigned char *to = static_cast<unsigned char *>(workspace);
-        if (const int rc = rnnt_mx4_quantize(a, a_type, M, K, a_stride, to, to + cb, nullptr, stream)) return rc;
-        args.a = to;
-        args.a_scales = to + cb;
-    }
     auto run = [&](auto shape, auto y) -> int {
         typedef decltype(shape) S;
         const auto kernel = mx4_tile_kernel<S, decltype(y)::value>;
         const int64_t mb = tiles(M, S::BM), nb = tiles(N, S::BN);
         if (mb * nb > kMostThreads / 256) return RNNT_ERR_UNSUPPORTED;
         MX4_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS));
+        if (!codes) {                                      // (the first that is queued, behind everything that may be refused)
+            int64_t cb = 0, sb = 0;
+            (void)rnnt_mx4_sizes(M, K, &cb, &sb);
+            unsigned char *to = static_cast<unsigned char *>(workspace);
+            if (const int rc = rnnt_mx4_quantize(a, a_type, M, K, a_stride, to, to + cb, nullptr, stream)) return rc;
+            args.a = to;
+            args.a_scales = to + cb;
+        }
         const int64_t groups = S::CHAIN ? std::min<int64_t>(mb * nb, kComputeUnits * S::GROUPS) : mb * nb;
         hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), S::LDS, on, args, (int)mb, (int)nb);
         MX4_TRY(hipGetLastError());

@@ -1,0 +1,24 @@
+"""What the operators decide on the host, no GPU needed: refusals before anything is queued, and arguments that a C
+integer would not hold."""
+import ctypes
+
+import pytest
+
+OK, NULL, SHAPE, HIP, UNSUPPORTED, SCRATCH = 0, -1, -2, -4, -5, -6
+P = 0x100000
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_2406_03791_amd as pkg
+    return pkg.load_library()
+
+
+@pytest.mark.parametrize("a_type", [0, 1, 2, 3])
+@pytest.mark.parametrize("M,N,K", [(1 << 24, 1 << 20, 512), (1 << 20, 1 << 24, 512), (1 << 24, 1 << 20, 128)])
+def test_a_product_of_too_many_blocks_is_refused_before_its_operand_is_quantised(lib, a_type, M, N, K):
+    """2^28 blocks and more of the result, a quantisation that is within its own limit: what has been queued by then would come
+    back as an error of the HIP runtime here, where there is no device."""
+    need = ctypes.c_int64(-1)
+    assert lib.rnnt_mx4_product_workspace(a_type, M, N, K, ctypes.byref(need)) == OK and (need.value > 0) == (a_type != 3)
+    assert lib.rnnt_mx4_product(P, P, a_type, K, P, P, None, P, 0, N, M, N, K, P, need.value, None) == UNSUPPORTED
