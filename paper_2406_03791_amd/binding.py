@@ -11,7 +11,7 @@ from typing import Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 
-RNNT_OK = 0
+RNNT_OK, RNNT_ERR_UNSUPPORTED = 0, -5
 RNNT_DEV_LEN_CLAMPED, RNNT_DEV_OVERFLOW, RNNT_DEV_ABORTED = 1, 2, 4
 
 EXPORTS = (
@@ -369,7 +369,15 @@ def rnnt_mx4_product(a, a_scales, a_type, a_stride, w_codes, w_scales, bias, y, 
                                            stream or None))
 
 
+def _counts(*counts) -> None:
+    """Refuses what an int32 argument does not hold: ctypes would cut it off."""
+    if any(not -0x80000000 <= n <= 0x7fffffff for n in counts):
+        raise RnntError(RNNT_ERR_UNSUPPORTED, f"a count of {counts} is beyond 32 bits")
+
+
 def rnnt_beam_select_workspace(B: int, beams: int, V: int, n_out: int) -> int:
+    if (B | beams | V | n_out) >> 31:
+        _counts(B, beams, V, n_out)
     out = C.c_int64(0)
     _check(load_library().rnnt_beam_select_workspace(B, beams, V, n_out, C.byref(out)))
     return out.value
@@ -377,6 +385,8 @@ def rnnt_beam_select_workspace(B: int, beams: int, V: int, n_out: int) -> int:
 
 def rnnt_beam_select(logits, type, batch_stride, beam_stride, scores, finished, B, beams, V, n_out, end_token,
                      scores_out, tokens_out, parents_out, workspace=None, workspace_bytes=0, stream: int = 0) -> None:
+    if (B | beams | V | n_out | end_token) >> 31:
+        _counts(B, beams, V, n_out, end_token)
     _check(load_library().rnnt_beam_select(_a(logits), type, batch_stride, beam_stride, _a(scores), _a(finished),
                                            B, beams, V, n_out, end_token, _a(scores_out), _a(tokens_out),
                                            _a(parents_out), _a(workspace), workspace_bytes, stream or None))
@@ -422,6 +432,8 @@ def rnnt_beam_states(pairs) -> BeamStates:
 
 def rnnt_beam_reorder(states, parents, B, beams_in, beams_out, stream: int = 0) -> None:
     """states: of rnnt_beam_states, to be used again as long as the tensors stay where they are."""
+    if (B | beams_in | beams_out) >> 31:
+        _counts(B, beams_in, beams_out)
     _check(load_library().rnnt_beam_reorder(states.array, len(states.pairs), _a(parents), B, beams_in, beams_out,
                                             stream or None))
 

@@ -22,3 +22,35 @@ def test_a_product_of_too_many_blocks_is_refused_before_its_operand_is_quantised
     need = ctypes.c_int64(-1)
     assert lib.rnnt_mx4_product_workspace(a_type, M, N, K, ctypes.byref(need)) == OK and (need.value > 0) == (a_type != 3)
     assert lib.rnnt_mx4_product(P, P, a_type, K, P, P, None, P, 0, N, M, N, K, P, need.value, None) == UNSUPPORTED
+
+
+WRAPS = 2 ** 32
+
+
+class _Address:
+    def data_ptr(self):
+        return P
+
+
+@pytest.mark.parametrize("by", [WRAPS, -WRAPS, 2 ** 31, 5 * WRAPS])
+def test_counts_that_a_32_bit_argument_does_not_hold_are_refused(by):
+    """Cut to 32 bits they would be ordinary calls: a vocabulary of 2^32 + 5 tokens one of 5.  (B = 0, so that a call that
+    is not refused has nothing to do.)"""
+    import paper_2406_03791_amd as pkg
+    a = _Address()
+    for at, few in ((0, 0), (1, 4), (2, 5), (3, 4)):
+        k = [0, 4, 5, 4]
+        k[at] = few + by
+        with pytest.raises(pkg.RnntError):
+            pkg.rnnt_beam_select_workspace(*k)
+        with pytest.raises(pkg.RnntError):
+            pkg.rnnt_beam_select(a, 0, 20, 5, a, None, *k, -1, a, a, a)
+    with pytest.raises(pkg.RnntError):
+        pkg.rnnt_beam_select(a, 0, 20, 5, a, a, 0, 4, 5, 4, 1 + by, a, a, a)
+    states = pkg.rnnt_beam_states([])
+    states.pairs, states.array = [None], (type(states.array)._type_ * 1)()
+    for k in ((by, 4, 4), (0, 4 + by, 4), (0, 4, 4 + by)):
+        with pytest.raises(pkg.RnntError):
+            pkg.rnnt_beam_reorder(states, a, *k)
+    pkg.rnnt_beam_reorder(states, a, 0, 4, 4)
+    pkg.rnnt_beam_select(a, 0, 20, 5, a, None, 0, 4, 5, 4, -1, a, a, a)
