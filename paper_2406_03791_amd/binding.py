@@ -561,6 +561,13 @@ def _on_device(first, *others):
     return first.device
 
 
+def _no_gradients(*tensors) -> None:
+    """Refuses operands that a gradient is to be recorded for: the operators have no backward pass."""
+    import torch
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError("an operand requires a gradient, and this operator has none: call it under torch.no_grad() or on detached tensors")
+
+
 def _workspace(given, need: int, device):
     """A workspace of at least `need` bytes and its size: the given one, or a new one."""
     import torch
@@ -603,6 +610,8 @@ class Mx4Matrix:
             raise ValueError(f"x is {tuple(x.shape)}, the matrix {(self.rows, self.cols)}")
         if values is not None and (values.dtype != torch.float32 or values.shape != x.shape or not values.is_contiguous()):
             raise ValueError("values: a contiguous float32 tensor of the matrix' size is wanted")
+        if values is not None:                             # (codes alone are integers)
+            _no_gradients(x, values)
         with torch.cuda.device(_on_device(x, self.codes, values)):
             rnnt_mx4_quantize(x, _type_of(x), self.rows, self.cols, stride, self.codes, self.scales, values,
                               torch.cuda.current_stream().cuda_stream)
@@ -620,6 +629,7 @@ class Mx4Matrix:
             raise ValueError(f"a has {cols} columns, the matrix {self.cols}")
         if bias is not None and (bias.dtype != torch.float32 or tuple(bias.shape) != (self.rows,) or not bias.is_contiguous()):
             raise ValueError("bias: a contiguous float32 vector of the matrix' rows is wanted")
+        _no_gradients(codes, bias, out)
         device = _on_device(codes, scales, self.codes, bias, out, workspace)
         if out is None:
             out = torch.empty((M, self.rows), dtype=dtype or torch.float32, device=device)
@@ -652,6 +662,7 @@ def beam_select(logits, scores, n_out: Optional[int] = None, finished=None, end_
     if finished is not None and (finished.dtype not in (torch.uint8, torch.bool) or tuple(finished.shape) != (B, beams)
                                  or not finished.is_contiguous()):
         raise ValueError("finished: a contiguous uint8 or bool tensor [B, beams] is wanted")
+    _no_gradients(logits, scores)
     device = _on_device(logits, scores, finished, workspace)
     workspace, space = _workspace(workspace, rnnt_beam_select_workspace(B, beams, V, n_out), device)
     best = torch.empty((B, n_out), dtype=torch.float32, device=device)
@@ -674,7 +685,9 @@ def beam_reorder(pairs, parents) -> None:
     if parents.dtype != torch.int32 or parents.dim() != 2 or not parents.is_contiguous():
         raise ValueError("parents: a contiguous int32 tensor [B, beams] is wanted")
     (B, beams_out), beams_in = parents.shape, states.pairs[0][0].shape[-2]
-    device = _on_device(parents, *[t for pair in states.pairs for t in pair])
+    moved = [t for pair in states.pairs for t in pair]
+    _no_gradients(*moved)
+    device = _on_device(parents, *moved)
     for src, dst in states.pairs:
         if tuple(src.shape[-3:-1]) != (B, beams_in) or tuple(dst.shape[-3:-1]) != (B, beams_out):
             raise ValueError(f"states of {B} utterances, {beams_in} and {beams_out} beams are wanted, not "

@@ -54,3 +54,30 @@ def test_counts_that_a_32_bit_argument_does_not_hold_are_refused(by):
             pkg.rnnt_beam_reorder(states, a, *k)
     pkg.rnnt_beam_reorder(states, a, 0, 4, 4)
     pkg.rnnt_beam_select(a, 0, 20, 5, a, None, 0, 4, 5, 4, -1, a, a, a)
+
+
+def test_operands_that_a_gradient_is_wanted_for_are_refused():
+    """There is no backward pass: a result without its gradient would train on without a word.  Refused before the tensors' device is
+    looked at, so that CPU tensors do; codes alone are integers, which have none, and without gradients recorded nothing is refused
+    for them (these calls go on to the refusal of tensors on the CPU)."""
+    import torch
+    import paper_2406_03791_amd as pkg
+    m = pkg.Mx4Matrix(3, 64, "cpu")
+    a, g = torch.zeros((2, 64)), torch.zeros((2, 64), requires_grad=True)
+    b, bg, y, yg = torch.zeros(3), torch.zeros(3, requires_grad=True), torch.zeros((2, 3)), torch.zeros((2, 3), requires_grad=True)
+    x, xg, v, vg = (torch.zeros((3, 64), requires_grad=r) for r in (False, True, False, True))
+    z, zg = (torch.zeros((1, 2, 5), requires_grad=r) for r in (False, True))
+    s, sg = (torch.zeros((1, 2), requires_grad=r) for r in (False, True))
+    p, h, hg = torch.zeros((1, 2), dtype=torch.int32), torch.zeros((1, 2, 5)), torch.zeros((1, 2, 5), requires_grad=True)
+    calls = [lambda: m.product(g), lambda: m.product(a, bias=bg), lambda: m.product(a, out=yg), lambda: m.product(g, bias=b, out=y),
+             lambda: m.product(2 * g), lambda: m.quantize(xg, values=v), lambda: m.quantize(x, values=vg),
+             lambda: pkg.beam_select(zg, s), lambda: pkg.beam_select(z, sg), lambda: pkg.beam_reorder([(hg, h)], p), lambda: pkg.beam_reorder([(h, hg)], p),
+             lambda: pkg.beam_reorder(pkg.rnnt_beam_states([(h, hg)]), p)]
+    for call in calls:
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+            call()
+    for call in (lambda: m.quantize(xg), lambda: pkg.mx4_quantize(xg), lambda: m.product(a), lambda: pkg.beam_select(z, s), lambda: pkg.beam_reorder([(h, h)], p)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
