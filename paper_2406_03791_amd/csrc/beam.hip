@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "engine.h"
+#include "wave.h"
 
 namespace rnnt {
 
@@ -122,13 +123,6 @@ template <int WIDTH, class Item> __device__ __forceinline__ Item reverse(const I
     const Item r = v.template lane<15>();
     if constexpr (WIDTH == 16) return r;
     else return r.template lane<16>().template lane<32>();
-}
-
-// What lanes of a wave wrote to LDS is there for the others
-__device__ __forceinline__ void wave_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
 }
 
 template <int TYPE> struct Logit;
@@ -690,14 +684,14 @@ beam_row_kernel(const SelectArgs a)
 // of a row and join their lists, two by two.
 constexpr int kScanWaves = 4;
 struct ScanLds { u64 buffers[kScanWaves][kBuffer]; double sums[kScanWaves], refs[kScanWaves]; };
-struct Piece { unsigned hyp, b; int from, to; };
-__device__ __forceinline__ Piece piece_of(const SelectArgs &a, int wave)
+struct ScanPiece { unsigned hyp, b; int from, to; };
+__device__ __forceinline__ ScanPiece piece_of(const SelectArgs &a, int wave)
 {
     const unsigned hyp = blockIdx.x / a.pieces;
     const long long piece = (long long)(blockIdx.x - hyp * a.pieces) * kScanWaves + wave;
     return {hyp, hyp / a.beams, (int)min(piece * a.piece_tiles * kTile, (long long)a.V), (int)min((piece + 1) * a.piece_tiles * kTile, (long long)a.V)};
 }
-__device__ __forceinline__ void store_piece(const SelectArgs &a, const ScanLds &lds, int lane, u64 key)
+__device__ __forceinline__ void store_list(const SelectArgs &a, const ScanLds &lds, int lane, u64 key)
 {
     if (lane < a.n_out) a.lists[(long long)blockIdx.x * a.n_out + lane] = key;
     if (lane < kScanWaves) { a.sums[(long long)blockIdx.x * kScanWaves + lane] = lds.sums[lane]; a.refs[(long long)blockIdx.x * kScanWaves + lane] = lds.refs[lane]; }
@@ -706,7 +700,7 @@ template <int TYPE, int WIDTH>
 __device__ __forceinline__ void scan_pieces(const SelectArgs &a, ScanLds &lds)
 {
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const Piece p = piece_of(a, wave);
+    const ScanPiece p = piece_of(a, wave);
     auto s = scan_of<typename Logit<TYPE>::T, WIDTH, true>(a, (int)p.b, (int)(p.hyp - p.b * a.beams), lds.buffers[wave]);
     s.begin(p.from, p.to);
     if ((a.finished && a.finished[p.hyp]) || !(a.scores[p.hyp] > -INFINITY)) return;       // (the whole work-group)
@@ -717,7 +711,7 @@ __device__ __forceinline__ void scan_pieces(const SelectArgs &a, ScanLds &lds)
         __syncthreads();
         if (wave < half) join<WIDTH>(s.list, InRow{lds.buffers[wave + half][WIDTH - 1 - lane % WIDTH]});
     }
-    if (wave == 0) store_piece(a, lds, lane, s.list.key);
+    if (wave == 0) store_list(a, lds, lane, s.list.key);
 }
 template <int TYPE, int WIDTH>
 __global__ void __launch_bounds__(kScanWaves * 64)
@@ -741,7 +735,7 @@ beam_held_kernel(const SelectArgs a)
     __shared__ unsigned group[64];
     __shared__ int found_count;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const Piece p = piece_of(a, wave);
+    const ScanPiece p = piece_of(a, wave);
     Held<T> h;
     h.row = static_cast<const T *>(a.logits) + p.b * a.batch_stride + (p.hyp - p.b * a.beams) * a.beam_stride + p.from;
     h.rest = p.to - p.from;
@@ -775,7 +769,7 @@ beam_held_kernel(const SelectArgs a)
         sort_lanes<64>(v);
         if constexpr (WIDTH == 16) v = v.template lane<16>().template lane<32>();     // the best 16, worst first, to lanes 0 .. 15
     }
-    store_piece(a, lds, lane, reverse<WIDTH>(v).key);
+    store_list(a, lds, lane, reverse<WIDTH>(v).key);
 }
 template <int WIDTH>
 __global__ void __launch_bounds__(kJoinWaves * 64)

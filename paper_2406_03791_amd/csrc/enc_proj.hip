@@ -3,6 +3,7 @@
 // first LSTM layer's input term.
 #include "engine.h"
 #include "parts.h"
+#include "wave.h"
 #include <type_traits>
 
 namespace rnnt {
@@ -40,13 +41,6 @@ __device__ __forceinline__ void init_call(const CallInit &ci, int B)
         if (ci.logps) ci.logps[i] = 0.f;
         if (ci.durs) ci.durs[i] = -1;
     }
-}
-
-__device__ __forceinline__ const char *uniform(const char *p)
-{
-    const unsigned long long u = reinterpret_cast<unsigned long long>(p);
-    const unsigned lo = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)u), hi = (unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32));
-    return reinterpret_cast<const char *>((unsigned long long)hi << 32 | lo);
 }
 
 // A wave's 32 rows of frames: tile number `tile` of the valid rows of all utterances, in tiles of an utterance's own.

@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "engine.h"
+#include "wave.h"
 
 namespace rnnt {
 
@@ -285,20 +286,6 @@ mx4_product_kernel(const ProductArgs g)
         o[e] = all[0] + (g.bias && n + e < g.N ? g.bias[n + e] : 0.f);
     }
     store_four(g.y, g.y_type, ((long long)mt * kTileRows + m) * g.y_stride + n, o, g.N - n);
-}
-
-// What lanes of a wave wrote to LDS is there for the others
-__device__ __forceinline__ void wave_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
-__device__ __forceinline__ const unsigned char *uniform(const unsigned char *p)
-{
-    const unsigned long long u = reinterpret_cast<unsigned long long>(p);
-    const unsigned lo = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)u), hi = (unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32));
-    return reinterpret_cast<const unsigned char *>((unsigned long long)hi << 32 | lo);
 }
 
 // Many rows: bound by the matrix instructions, 32 cycles for 32 x 32 x 64 (and, in long products, by what the card may draw: those

@@ -81,3 +81,29 @@ def test_operands_that_a_gradient_is_wanted_for_are_refused():
     for call in (lambda: m.quantize(xg), lambda: pkg.mx4_quantize(xg), lambda: m.product(a), lambda: pkg.beam_select(z, s), lambda: pkg.beam_reorder([(h, h)], p)):
         with pytest.raises(ValueError, match="GPU"):
             call()
+
+
+def test_what_two_sources_define_in_one_namespace_has_one_name_each():
+    """Two definitions of one name in a namespace that units share break C++'s rule of one definition, whatever the linker makes of
+    it; what both need is in a header."""
+    import collections
+    import os
+    import re
+    import paper_2406_03791_amd as pkg
+    folder = os.path.join(os.path.dirname(pkg.__file__), "csrc")
+    where = collections.defaultdict(set)
+    for name in sorted(os.listdir(folder)):
+        shared = False
+        with open(os.path.join(folder, name)) as f:
+            for line in f:
+                if re.match(r"(}  // )?namespace", line):
+                    shared = line.startswith("namespace rnnt")
+                if not shared or line.rstrip().endswith(";"):
+                    continue
+                m = (re.match(r"(?:template <(?!>).*?> )?(?:struct|class|union|enum) (\w+)", line)
+                     or re.match(r"(?:template <.*> )?(?:(?:__\w+__|static|inline|constexpr) )+[\w :]*?[\w>&*] ?[&*]?\b(?!__)(\w+)\(.*\)\s*(?:\{.*)?$", line))
+                if m:
+                    where[m.group(1)].add(name)
+    assert "wave_sync" in where and "SelectArgs" in where and "aligned" not in where
+    twice = {k: v for k, v in where.items() if len(v) > 1}
+    assert not twice, twice
