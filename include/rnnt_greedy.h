@@ -639,7 +639,9 @@ int rnnt_mx4_product(const void *a, const void *a_scales, int32_t a_type, int64_
  * A step of a beam search: the n_out best continuations of every utterance.  The
  * candidate (k, v), token v behind hypothesis k, has the score
  *   scores[b, k] + logits[b, k, v] - log(sum over u of exp(logits[b, k, u])),
- * added up in 64 bits, the sum's terms in 32.  Candidates of an utterance go by their score, those of one
+ * added up in 64 bits, the sum's terms in 32: its logarithm is off by less than
+ * (2.25 ln V + 11.5) 2^-24, 1.6e-6 for 1025 tokens and 2.2e-6 for 65535, and hypotheses whose
+ * candidates are nearer than that of both may change places.  Candidates of an utterance go by their score, those of one
  * hypothesis by their logit, and what ties by the lower k, then the lower v.
  *   logits   [B, beams, V] of `type` (F32, BF16 or F16), strides in elements (>= 0; 0: the
  *            same for all); a logit of -inf is no candidate

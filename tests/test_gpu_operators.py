@@ -33,3 +33,45 @@ def test_sums_of_rows_that_rise_all_along(pkg, B, V, n, rise):  # noqa: F811
     want = scores.double().numpy() + d.max() - total
     off = float(np.abs(s.double().cpu().numpy() - want).max())
     assert off <= 2.0 ** -21
+
+
+# an utterance in one launch without lists (one and two rows a wave), with lists, rows held whole, in pieces, in pieces by lists, and lists of many rows
+ORDERS = [(3, 8, 300, 8), (2, 20, 1025, 30), (2, 40, 1025, 40), (3, 4, 4097, 4), (2, 3, 40000, 9), (2, 3, 40000, 40), (1400, 3, 2000, 33)]
+
+
+def _ordered(pkg, x, scores, n, finished=None, end=0):  # noqa: F811
+    from operators_order import check_order
+    got = pkg.beam_select(x.cuda(), scores.cuda(), n, None if finished is None else finished.cuda(), end)
+    check_order(tuple(t.cpu().numpy() for t in got), x.double().numpy(), scores.double().numpy(), n, None if finished is None else finished.numpy(), end)
+
+
+@pytest.mark.parametrize("B,beams,V,n", ORDERS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_orders_where_scores_lose_the_logits(pkg, B, beams, V, n, dtype):  # noqa: F811
+    """Scores so large that all candidates of a hypothesis have the same: the hypothesis goes first, then the logit, then the token; and
+    scores that lose a part of the logits, or none."""
+    import torch
+    g = torch.Generator().manual_seed(V + n)
+    x = torch.randn((B, beams, V), generator=g) * 2
+    x[:, :, V // 2:] = torch.randint(-4, 4, (B, beams, V - V // 2), generator=g).float()     # many ties
+    x[0, 0, ::2] = -float("inf")
+    x = x.to(_torch_type(dtype))
+    finished = torch.rand((B, beams), generator=g) < 0.3
+    for value in (-1e30, -1e10, -3.0):
+        scores = torch.full((B, beams), value)
+        _ordered(pkg, x, scores, n)
+        _ordered(pkg, x, scores, n, finished, V - 1)
+        scores[:, 1] = 1.1 * value
+        scores[B - 1, beams - 1] = 0.9 * value
+        _ordered(pkg, x, scores, n)
+
+
+@pytest.mark.parametrize("B,beams,V,n", ORDERS[:-1])
+def test_many_equal_logits_below_the_largest_one(pkg, B, beams, V, n):  # noqa: F811
+    """All terms of the sum but one are off by the same: what the logarithm may be off by is nearly reached here."""
+    import torch
+    g = torch.Generator().manual_seed(V)
+    for top in (0.0, 5.37, -811.3):
+        x = torch.full((B, beams, V), top) - (3 + 9 * torch.rand((B, beams, 1), generator=g))
+        x[:, :, V - 3] = top
+        _ordered(pkg, x, -torch.rand((B, beams), generator=g), n)
