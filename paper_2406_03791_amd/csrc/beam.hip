@@ -948,16 +948,19 @@ namespace {
 constexpr int64_t kMostThreads = 0xffffffff;                                // of a launch, at most
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
-// How a selection is cut up.  One launch, a work-group an utterance: short rows; rows that a wave holds as a whole, where that leaves a work-group
-// no more than kOneRowTiles tiles or there are kOneRowRows rows, and its waves few winners to rank; and by lists, where a wave has no
+// How a selection is cut up.  One launch, a work-group an utterance: short rows; rows that a wave holds as a whole, where there are few winners
+// for each of its waves to rank, and no more than kOneRowTiles tiles a work-group or kOneRowUtterances of them; and by lists, where a wave has no
 // more than kOneLaunchTiles tiles, of fewer than kWavesWanted rows that could be held in pieces kFewTiles: the second launch costs what a wave takes
 // for several tiles.  Else pieces of two tiles or more, towards sixteen waves on every compute unit; lists in pieces of fewer than kWavesWanted rows only.
-// us, bf16, rows held whole and in pieces: 1 x 4 rows of 4097 logits for 4 winners 7.5 and 8.7, 128 x 16 for 16 15.5 and 23, 1024 x 4 of 8192 for 4 18
-// and 26, 8 x 8 of 3000 for 8 8.7 and 9.1, but 16 x 16 of 4097 for 16 13.5 and 12.4, 64 x 16 of 8000 17.4 and 14.5, 1 x 2 of 3000 fp32 for 30 11.4 and 8.8,
-// 4096 x 2 of 1025 for 8 21.3 (lists 18.6).
+// us of the kernels, bf16, rows held whole and the other way (pieces, or lists where rows are two tiles or 4096).  Tiles: 16 x 16 rows of 4097
+// for 16 12.2 and 12.9, 64 x 16 12.5 and 16.5, 16 x 16 of 6000 12.4 and 12.2, 512 x 16 28.9 and 52.9; beyond kOneRowTiles 16 x 16 of 8000 13.8 and 12.1,
+// 48 x 16 of 8192 14.5 and 14.4, 64 x 16 of 8000 14.5 and 15.4, 256 x 16 18.0 and 30.6.  Winners a wave, kRowWinners = 4: one row of 4097 for 4 6.9 and 7.5,
+// for 8 9.1 and 8.1; 64 x 2 of 4097 for 8 8.8 and 9.7, for 16 11.3 and 10.5; 4096 x 2 of 8000 for 8 33.5 and 53.9, for 16 40.3 and 58.8; 64 x 4 of 4097
+// for 16 10.4 and 11.1, for 24 12.6 and 11.8; 64 x 8 of 8192 for 32 14.6 and 13.0, 300 x 8 21.0 and 29.6.  Of one or two rows that are short, where lists are one tile's,
+// as many winners a wave as there are waves: one of 1025 for one 4.6 and 4.8, for 2 5.3 and 4.8; 128 x 2 for 4 6.3 and 6.4, for 8 7.3 and 6.4.
 // By lists and in pieces: 128 x 20 of 4000 for 20 28.6 and 22.6, 8 x 32 of 2000 for 32 32 and 14.7, 512 x 4 of 65537 for 4 69 and 54, but
 // 128 x 32 of 2000 for 32 32 and 34.
-constexpr int kOneLaunchTiles = 8, kOneRowTiles = 64, kOneRowRows = 2048, kFewTiles = 2, kWavesWanted = 4096, kMostPieces = 64 / kScanWaves;
+constexpr int kOneLaunchTiles = 8, kOneRowTiles = 96, kOneRowUtterances = 48, kRowWinners = 4, kFewTiles = 2, kWavesWanted = 4096, kMostPieces = 64 / kScanWaves;
 
 struct SelectPlan {
     bool two = false, is_short = false, one_row = false, held = false;
@@ -973,7 +976,8 @@ struct SelectPlan {
         // (rows that waves hold as a whole: in no more pieces than the join takes)
         const int most = (type == RNNT_TYPE_F32 ? held_size<float>() : held_size<__bf16>()) / kTile;
         held = n <= kHeldWinners && V >= 8 && (row + most * kScanWaves - 1) / (most * kScanWaves) <= kMostPieces;
-        one_row = !is_short && held && row <= most && beams <= kJoinWaves && n <= waves * std::min(waves, 4) && (row * waves <= kOneRowTiles || B * beams >= kOneRowRows);
+        one_row = !is_short && held && row <= most && beams <= kJoinWaves && n <= waves * (V > kShortRow ? kRowWinners : waves) &&
+                  (row * waves <= kOneRowTiles || B >= kOneRowUtterances);
         if (is_short || one_row || (beams + waves - 1) / waves * row <= (held && B * beams < kWavesWanted ? kFewTiles : kOneLaunchTiles) || (!held && B * beams >= kWavesWanted)) return;
         two = true;
         const int64_t into = std::min<int64_t>(std::max<int64_t>(kWavesWanted / (B * beams * kScanWaves), 1), std::min(kMostPieces, (row + 2 * kScanWaves - 1) / (2 * kScanWaves)));

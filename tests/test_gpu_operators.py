@@ -176,3 +176,17 @@ def test_states_within_themselves_beside_others_in_one_call(pkg, beams):  # noqa
     for i, (h, d, o) in enumerate(zip(host, dev, to)):
         assert np.array_equal(o.cpu().numpy(), _moved(h, p)), (i, h.shape)
         assert i % 2 == 0 or np.array_equal(d.cpu().numpy(), h)
+
+
+@pytest.mark.parametrize("B,beams,V,n", [(3, 1, 1500, 4), (3, 1, 1500, 5), (2, 1, 1025, 1), (2, 1, 1025, 2), (3, 2, 8192, 8), (3, 2, 8192, 9), (3, 2, 1088, 4), (3, 2, 1088, 5),
+                                         (2, 4, 5000, 16), (2, 4, 5000, 17), (3, 16, 6144, 16), (3, 16, 6145, 16), (47, 16, 8000, 16), (48, 16, 8000, 16), (48, 9, 8193, 9)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_where_rows_begin_to_be_held_whole(pkg, B, beams, V, n, dtype):  # noqa: F811
+    """Both sides of what the way of a selection is chosen by: winners a wave, tiles a work-group, utterances."""
+    import torch
+    g = torch.Generator().manual_seed(B + V + n)
+    x = (torch.randn((B, beams, V), generator=g) * 2).to(_torch_type(dtype))
+    scores = -torch.rand((B, beams), generator=g)
+    _ordered(pkg, x, scores, n)
+    x[:, 0, V // 3:] = -float("inf")
+    _ordered(pkg, x, scores, n, torch.rand((B, beams), generator=g) < 0.3, V - 1)
