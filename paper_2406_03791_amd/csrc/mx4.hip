@@ -288,8 +288,9 @@ mx4_product_kernel(const ProductArgs g)
     store_four(g.y, g.y_type, ((long long)mt * kTileRows + m) * g.y_stride + n, o, g.N - n);
 }
 
-// Many rows: bound by the matrix instructions, 32 cycles for 32 x 32 x 64 (and, in long products, by what the card may draw: those
-// instructions alone, on random codes, reach 6.6 PFLOP/s here, on zeros 9.5).  A block of y, BM x BN outputs, is that of 2 x 2 waves
+// Many rows: bound by the matrix instructions, 32 cycles for 32 x 32 x 64, and by the schedule around them: they fill 51 % of the 515 000 cycles of a
+// product of 8192^3, whatever the codes.  (In long products the clock falls, too, to 1.75 - 1.95 GHz on random codes, 2.3 - 2.4 on
+// zeros: 258 - 287 us and 216 - 227; those instructions alone reach 6.6 PFLOP/s on random codes, on zeros 9.5.)  A block of y, BM x BN outputs, is that of 2 x 2 waves
 // with TM x TN tiles of 32 x 32 each.  Tiles of codes lie in memory as the lanes take them: they go to LDS in pieces of 1 KB, STAGES
 // tiles of K in turn, and from there to registers without bank conflicts.
 //
