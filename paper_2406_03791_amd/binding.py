@@ -622,8 +622,8 @@ class Mx4Matrix:
         `out`.  a: a tensor [M, cols] or an Mx4Matrix.  workspace: a uint8 tensor to be used instead of a new one."""
         import torch
         quantised = isinstance(a, Mx4Matrix)
-        M, cols = (a.rows, a.cols) if quantised else tuple(a.shape)
-        stride, a_type = (cols, RNNT_TYPE_MX4) if quantised else (_rows_of(a, "a"), _type_of(a))
+        stride, a_type = (a.cols, RNNT_TYPE_MX4) if quantised else (_rows_of(a, "a"), _type_of(a))
+        M, cols = (a.rows, a.cols) if quantised else a.shape
         codes, scales = (a.codes, a.scales) if quantised else (a, None)
         if cols != self.cols:
             raise ValueError(f"a has {cols} columns, the matrix {self.cols}")
@@ -645,6 +645,7 @@ class Mx4Matrix:
 
 def mx4_quantize(x) -> Mx4Matrix:
     """A new microscaled 4-bit copy of a matrix."""
+    _rows_of(x, "x")
     return Mx4Matrix(x.shape[0], x.shape[1], x.device).quantize(x)
 
 

@@ -107,3 +107,13 @@ def test_what_two_sources_define_in_one_namespace_has_one_name_each():
     assert "wave_sync" in where and "SelectArgs" in where and "aligned" not in where
     twice = {k: v for k, v in where.items() if len(v) > 1}
     assert not twice, twice
+
+
+def test_what_is_no_matrix_is_refused_as_such():
+    import torch
+    import paper_2406_03791_amd as pkg
+    m = pkg.Mx4Matrix(3, 64, "cpu")
+    for shape in ((), (64,), (1, 2, 64)):
+        for call in (lambda: pkg.mx4_quantize(torch.zeros(shape)), lambda: m.quantize(torch.zeros(shape)), lambda: m.product(torch.zeros(shape))):
+            with pytest.raises(ValueError, match="matrix"):
+                call()
